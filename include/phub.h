@@ -417,6 +417,143 @@ int phub_step_noalloc(int num_workers, int num_keys, const int64_t *key_elems,
                       int nesterov, const float *const *grads, float *weights, float *moments,
                       void *hip_stream);
 
+/* --------------------------------------------------------------------------
+ * The worker's operators: the end of a training worker's pass, where the
+ * loss is and the gradients that it pushes begin.  Weight gradients are fp32,
+ * the type that phub_push takes, and go where the caller says, such as
+ * the buffer of a key; with `accumulate` they are added to what is there
+ * (several micro-batches before one push).  Layer norm's weights are the fp32
+ * values that phub_pull hands out.
+ *
+ * Like phub_step_noalloc, each works on the caller's memory, on hip_stream
+ * (NULL = the null stream) of the current GPU, allocates nothing and does not
+ * wait for the stream.  All may be captured into a graph.  A `workspace` is
+ * device memory aligned to 256 bytes whose contents do not matter before or
+ * after a call; calls that share one must be ordered on one stream, and so
+ * must graphs that were captured with it.  Outputs must not overlap inputs or
+ * each other.  Every call gives the same bits for the same arguments.
+ *
+ * Matrices are row-major with rows `..._stride` elements apart (at least the
+ * number of columns) and aligned to their elements; 16-bit matrices whose
+ * rows all begin on 16-byte boundaries and have a multiple of 8 columns are
+ * read in place, others are copied first where products are made of them.  Zero rows
+ * are allowed (weight gradients are then cleared, or kept with `accumulate`).
+ * Errors: PHUB_EINVAL, PHUB_EHIP.
+ * ------------------------------------------------------------------------ */
+
+/* Element types of hidden states, their gradients and the vocabulary's
+ * weights.  Sums and statistics are fp32 for all of them. */
+enum phub_type { PHUB_F32 = 0, PHUB_BF16 = 1, PHUB_F16 = 2 };
+
+/*
+ * phub_layer_norm - for each of `rows` rows of `cols` columns
+ *     mean = sum x / cols,   rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps)
+ *     y    = (x - mean) rstd weight + bias
+ *   x, y          rows x cols of `type` (a phub_type).
+ *   weight, bias  cols values; NULL: ones, zeros.
+ *   mean, rstd    receive a value for each row (the backward pass takes
+ *                 them); either may be NULL.
+ * 0 <= rows < 2^30, 1 <= cols <= 2^20, eps >= 0 and finite.
+ */
+int phub_layer_norm(int type, int64_t rows, int64_t cols, const void *x, int64_t x_stride,
+                    const float *weight, const float *bias, float eps, void *y, int64_t y_stride,
+                    float *mean, float *rstd, void *hip_stream);
+
+/* phub_layer_norm_grad_bytes - bytes of workspace that
+ * phub_layer_norm_grad takes. */
+int phub_layer_norm_grad_bytes(int64_t rows, int64_t cols, int64_t *bytes);
+
+/*
+ * phub_layer_norm_grad - the gradients of phub_layer_norm for dy, y's: with
+ * h = (x - mean) rstd
+ *     dx      = rstd (dy weight - mean(dy weight) - h mean(dy weight h))
+ *     dweight = sum over rows of dy h,   dbias = sum over rows of dy
+ *   x, weight, mean, rstd   as given to and by phub_layer_norm.
+ *   dx, dweight, dbias      each may be NULL: not wanted.
+ *   workspace               needed for dweight or dbias.
+ */
+int phub_layer_norm_grad(int type, int64_t rows, int64_t cols, const void *dy, int64_t dy_stride,
+                         const void *x, int64_t x_stride, const float *weight, const float *mean,
+                         const float *rstd, void *dx, int64_t dx_stride, float *dweight,
+                         float *dbias, int accumulate, void *workspace, int64_t workspace_bytes,
+                         void *hip_stream);
+
+/*
+ * phub_vocab_bytes - bytes of workspace for the four functions below:
+ * *least, the fewest that a call takes, and *best, as many as it has use for
+ * (either may be NULL).  With fewer than *best the vocabulary is done in more
+ * pieces.
+ *   top   the teacher's entries a row, 0 for phub_vocab_loss.
+ *   grad  nonzero for the backward pass, with dx or dw or both wanted.
+ * Of x and w only the alignment counts; other arguments as below.
+ */
+int phub_vocab_bytes(int type, int64_t rows, int64_t cols, int64_t vocab, const void *x,
+                     int64_t x_stride, const void *w, int64_t w_stride, int top, int grad,
+                     int64_t *least, int64_t *best);
+
+/*
+ * phub_vocab_loss - softmax cross entropy of each row's target over a
+ * vocabulary, without keeping the rows x vocab logits z = x w^T:
+ *     lse = log sum over v of exp z_v,   loss = lse - z_target
+ *   x         rows x cols hidden states of `type`.
+ *   w         vocab x cols weights of the same type.
+ *   target    a vocabulary row for each row of x.  A row whose target is
+ *             outside [0, vocab) (padding) has loss 0 and no gradient,
+ *             whatever its hidden states hold.
+ *   loss, lse receive a value for each row.
+ * 0 <= rows <= 2^22, 1 <= cols <= 2^16, 1 <= vocab <= 2^24, strides at most
+ * 2^22.  A vector of biases can be a column of w that meets a column of ones
+ * in x.
+ */
+int phub_vocab_loss(int type, int64_t rows, int64_t cols, int64_t vocab, const void *x,
+                    int64_t x_stride, const void *w, int64_t w_stride, const int64_t *target,
+                    float *loss, float *lse, void *workspace, int64_t workspace_bytes,
+                    void *hip_stream);
+
+/*
+ * phub_vocab_loss_grad - the gradients of sum over rows of dloss loss:
+ *     G = dloss (softmax(z) - [v = target]),   dx = G w,   dw = G^T x
+ *   lse    as written by phub_vocab_loss for the same arguments.
+ *   dloss  a value for each row; NULL: ones.
+ *   dx     rows x cols of `type`; NULL: not wanted.
+ *   dw     vocab x cols fp32; NULL: not wanted.
+ */
+int phub_vocab_loss_grad(int type, int64_t rows, int64_t cols, int64_t vocab, const void *x,
+                         int64_t x_stride, const void *w, int64_t w_stride, const int64_t *target,
+                         const float *lse, const float *dloss, void *dx, int64_t dx_stride,
+                         float *dw, int64_t dw_stride, int accumulate, void *workspace,
+                         int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * phub_distill_loss - each row's divergence from a teacher of which `top`
+ * logits are known, at `temperature` T, over the same logits z = x w^T:
+ *     q    = softmax(logit / T) over the row's entries
+ *     lse  = log sum over v of exp(z_v / T)
+ *     loss = T^2 sum over entries of q (log q - z_index / T + lse)
+ *   index, logit  rows x top, contiguous.  Entries with an index outside
+ *                 [0, vocab) or a logit of -infinity are absent; entries of
+ *                 one row with the same index add up to one.  A row without
+ *                 entries has loss 0 and no gradient.
+ * 1 <= top <= 1024, T finite and > 0; other arguments and limits as
+ * phub_vocab_loss.
+ */
+int phub_distill_loss(int type, int64_t rows, int64_t cols, int64_t vocab, const void *x,
+                      int64_t x_stride, const void *w, int64_t w_stride, int top,
+                      const int64_t *index, const float *logit, float temperature, float *loss,
+                      float *lse, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * phub_distill_loss_grad - the gradients of sum over rows of dloss loss:
+ *     G = dloss T (softmax(z / T) - q),   dx = G w,   dw = G^T x
+ * Arguments as phub_vocab_loss_grad and phub_distill_loss.
+ */
+int phub_distill_loss_grad(int type, int64_t rows, int64_t cols, int64_t vocab, const void *x,
+                           int64_t x_stride, const void *w, int64_t w_stride, int top,
+                           const int64_t *index, const float *logit, float temperature,
+                           const float *lse, const float *dloss, void *dx, int64_t dx_stride,
+                           float *dw, int64_t dw_stride, int accumulate, void *workspace,
+                           int64_t workspace_bytes, void *hip_stream);
+
 /* Message of the last failed call on this thread ("" if none).  The string
  * belongs to the library and lives until the thread's next failing call. */
 const char *phub_last_error(void);

@@ -32,9 +32,10 @@ ROOTS_LIB = os.path.join(PKG, "libphub_roots.so")
 ROOTS_SOURCES = ["roots.hip"]
 
 SOURCES = ["plan.cpp", "phub_api.cpp", "fused_step.hip", "fused_stream.hip", "fused_many.hip",
-           "fused_many_shared.hip", "put_pointers.hip", "step_noalloc.hip"]
+           "fused_many_shared.hip", "put_pointers.hip", "step_noalloc.hip", "worker_api.cpp",
+           "layer_norm.hip", "vocab_loss.hip"]
 HEADERS = ["plan.hpp", "kernels.hpp", "device.hpp", "tile_walk.hpp", "stream_walk.hpp",
-           "many_walk.hpp"]
+           "many_walk.hpp", "worker_ops.hpp", "elements.hpp", "products.hpp"]
 # Sources that hold many kernels, and the parts (PHUB_STEP_PART) that they are
 # compiled in
 PARTS = {"fused_step.hip": range(8), "fused_stream.hip": range(0, 8, 2)}

@@ -45,6 +45,15 @@ def load_library(path: Optional[str] = None) -> _phub.Library:
     return _phub.load(path)
 
 
+class _Pulled:
+    """A key's weights in the job's memory, for torch."""
+
+    def __init__(self, job, ptr, n):
+        self.job = job
+        self.__cuda_array_interface__ = {"shape": (n,), "typestr": "<f4", "data": (ptr, False),
+                                         "strides": None, "version": 2}
+
+
 class TorchJob:
     """A phub job plus the torch buffers of its N workers.
 
@@ -159,6 +168,22 @@ class TorchJob:
         keys, ptrs = bucket
         self.lib.phub_push_keys_event(self.handle, worker, ptrs, keys,
                                       None if event is None else event.cuda_event)
+
+    def gradient(self, worker: int, key: int, *shape: int):
+        """Key ``key`` in worker ``worker``'s attached arena, as a tensor of
+        ``shape`` (default: flat): where an operator writes the gradient that
+        the worker pushes."""
+        o, n = self.offsets[key], self.spec.key_elems[key]
+        return self._grad_refs[worker][o:o + n].view(shape or (n,))
+
+    def weights(self, key: int, *shape: int):
+        """Key ``key``'s weights as phub_pull hands them out, as a tensor of
+        ``shape`` (default: flat) that shares the job's memory and is read
+        only: ordered after earlier steps on the job's stream, changed by the
+        next step, gone with the job (which the tensor keeps)."""
+        n = self.spec.key_elems[key]
+        ptr = self.lib.phub_pull(self.handle, key)
+        return self.torch.as_tensor(_Pulled(self, ptr, n), device=self.device).view(shape or (n,))
 
     def attach_models(self, worker: int, arena) -> None:
         """Use ``arena`` (arena_elems fp32 values) as worker ``worker``'s model

@@ -34,6 +34,10 @@ PHUB_SCHEDULE_DYNAMIC = 2
 PHUB_OPT_MOMENTUM = 0
 PHUB_OPT_SGD = 1
 PHUB_OPT_ADAM = 2
+PHUB_F32 = 0
+PHUB_BF16 = 1
+PHUB_F16 = 2
+
 OPTIMIZERS = {"momentum": PHUB_OPT_MOMENTUM, "sgd": PHUB_OPT_SGD, "adam": PHUB_OPT_ADAM}
 
 # Every symbol the header declares.
@@ -43,7 +47,10 @@ EXPORTED = ("phub_init", "phub_init_ex", "phub_set_weights", "phub_push", "phub_
             "phub_step", "phub_pull", "phub_get_state", "phub_get_second_moment", "phub_sync",
             "phub_get_stream",
             "phub_job_info", "phub_destroy", "phub_last_error", "phub_plan_count",
-            "phub_plan_build", "phub_step_noalloc")
+            "phub_plan_build", "phub_step_noalloc",
+            "phub_layer_norm", "phub_layer_norm_grad_bytes", "phub_layer_norm_grad",
+            "phub_vocab_bytes", "phub_vocab_loss", "phub_vocab_loss_grad",
+            "phub_distill_loss", "phub_distill_loss_grad")
 
 
 class PhubError(RuntimeError):
@@ -74,6 +81,8 @@ class Library:
         lib = ctypes.CDLL(path)
         vp, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float
         pp = ctypes.POINTER(ctypes.c_void_p)
+        products = [i64, i64, i64, vp, i64, vp, i64]  # rows, cols, vocab, x and w with strides
+        gradients = [vp, i64, vp, i64, i32, vp, i64, vp]  # dx and dw with strides ... stream
         sig = {
             "phub_init": ([pp, i32, i32, vp, i64, f32, f32, f32, i32, vp], i32),
             "phub_init_ex": ([pp, i32, i32, vp, i64, f32, f32, f32, i32, vp,
@@ -100,6 +109,16 @@ class Library:
                                  ctypes.POINTER(i32), ctypes.POINTER(i64)], i32),
             "phub_plan_build": ([i32, i32, vp, i64, i32, i32, i32, vp, vp, vp], i32),
             "phub_step_noalloc": ([i32, i32, vp, i64, f32, f32, f32, i32, vp, vp, vp, vp], i32),
+            "phub_layer_norm": ([i32, i64, i64, vp, i64, vp, vp, f32, vp, i64, vp, vp, vp], i32),
+            "phub_layer_norm_grad_bytes": ([i64, i64, ctypes.POINTER(i64)], i32),
+            "phub_layer_norm_grad": ([i32, i64, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp,
+                                      i32, vp, i64, vp], i32),
+            "phub_vocab_bytes": ([i32, i64, i64, i64, vp, i64, vp, i64, i32, i32,
+                                  ctypes.POINTER(i64), ctypes.POINTER(i64)], i32),
+            "phub_vocab_loss": ([i32, *products, vp, vp, vp, vp, i64, vp], i32),
+            "phub_vocab_loss_grad": ([i32, *products, vp, vp, vp, *gradients], i32),
+            "phub_distill_loss": ([i32, *products, i32, vp, vp, f32, vp, vp, vp, i64, vp], i32),
+            "phub_distill_loss_grad": ([i32, *products, i32, vp, vp, f32, vp, vp, *gradients], i32),
         }
         for name, (args, res) in sig.items():
             fn = getattr(lib, name)
@@ -270,6 +289,36 @@ class Library:
             int(num_workers), len(key_elems), elems, int(chunk_bytes), float(lr), float(momentum),
             float(weight_decay), int(bool(nesterov)), grad_ptrs, weights_ptr,
             moments_ptr, stream), check)
+
+    # -- the worker's operators (pointers as ints; see phub.h) ---------------
+    def phub_layer_norm(self, *args, check: bool = True) -> int:
+        return self._check(self.lib.phub_layer_norm(*args), check)
+
+    def phub_layer_norm_grad_bytes(self, rows: int, cols: int) -> int:
+        out = ctypes.c_int64()
+        self._check(self.lib.phub_layer_norm_grad_bytes(int(rows), int(cols), ctypes.byref(out)), True)
+        return out.value
+
+    def phub_layer_norm_grad(self, *args, check: bool = True) -> int:
+        return self._check(self.lib.phub_layer_norm_grad(*args), check)
+
+    def phub_vocab_bytes(self, *args):
+        """(least, best) bytes of workspace."""
+        least, best = ctypes.c_int64(), ctypes.c_int64()
+        self._check(self.lib.phub_vocab_bytes(*args, ctypes.byref(least), ctypes.byref(best)), True)
+        return least.value, best.value
+
+    def phub_vocab_loss(self, *args, check: bool = True) -> int:
+        return self._check(self.lib.phub_vocab_loss(*args), check)
+
+    def phub_vocab_loss_grad(self, *args, check: bool = True) -> int:
+        return self._check(self.lib.phub_vocab_loss_grad(*args), check)
+
+    def phub_distill_loss(self, *args, check: bool = True) -> int:
+        return self._check(self.lib.phub_distill_loss(*args), check)
+
+    def phub_distill_loss_grad(self, *args, check: bool = True) -> int:
+        return self._check(self.lib.phub_distill_loss_grad(*args), check)
 
     # -- schedule (host only) ----------------------------------------------
     def phub_plan_count(self, num_workers: int, key_elems: Sequence[int], chunk_bytes: int,
