@@ -18,15 +18,17 @@
 //
 // Tiles travel from memory to LDS without passing registers (16 bytes a lane), through
 // buffer descriptors that end with the tile's last row: rows and k beyond
-// the operand read as zero.  LDS rows are 128 bytes, the 16-byte pieces of row
-// r stored in the order piece ^ (r % 8), so that eight neighbouring rows'
-// pieces lie in different banks; a wave's load writes LDS in lane order, so
-// the order is made by which piece each lane asks for.
+// the operand read as zero.  The 16-byte pieces of an LDS row are stored in an order
+// that depends on the row, so that one piece of sixteen neighbouring rows
+// lies in all 64 banks (an order that is right for 32 banks read at half the
+// rate); a wave's load writes LDS in lane order, so the order is made by
+// which piece each lane asks for.
 #pragma once
 
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "elements.hpp"
 
@@ -74,13 +76,18 @@ __device__ __forceinline__ f32x16 mfma(fp16x8 a, fp16x8 b, f32x16 c) {
 #define PHUB_LDS_PTR __attribute__((address_space(3)))
 
 constexpr int kProductThreads = 256;
-constexpr int kStepK = 64;  // k of one stage: an LDS row of 128 bytes
 
+// k of one stage: 32 for the largest tiles, whose products hide the latency of
+// LDS and the barrier of a stage; the smaller the tile, the longer its stage.
+// Measured with one tile a compute unit, D from 1024 to 4096: 64 x 64 tiles
+// KSMALL us for 128 of k (1.1 with 32 a stage), 128 x 128 tiles KMID us for 64 (0.65).
 template <int WR, int WC>
 struct TileShape {
-    static constexpr int kR = 64 * WR, kC = 64 * WC;             // rows of the tile
-    static constexpr int kStageBytes = (kR + kC) * kStepK * 2;
-    static constexpr int kLoads = (kR + kC) / 32;                // 1 KiB loads of a wave for a stage
+    static constexpr int kR = 64 * WR, kC = 64 * WC;  // rows of the tile
+    static constexpr int kStepK = WR >= 4 ? 32 : WR == 2 ? 64 : 128;
+    static constexpr int kRowBytes = kStepK * 2;      // of LDS
+    static constexpr int kStageBytes = (kR + kC) * kRowBytes;
+    static constexpr int kLoads = kStageBytes / 4096;  // 1 KiB loads of a wave for a stage
 };
 
 // Place of a block: its tile and its part of the k loop.  Blocks go to the 8
@@ -125,7 +132,9 @@ __device__ __forceinline__ void multiply(const Product& p, const Place& at, char
                                          f32x16 (&acc)[WR][WC]) {
     typedef TileShape<WR, WC> S;
     typedef typename Frag<T>::type F;
-    constexpr int LR = S::kR / 32, LC = S::kC / 32;  // loads of a wave for each operand
+    constexpr int LR = S::kR * S::kRowBytes / 4096;  // loads of a wave that are R's
+    constexpr int kStepK = S::kStepK, kPieces = kStepK / 8;  // pieces of an LDS row
+    constexpr int kRowsOfLoad = 64 / kPieces;
     const int lane = int(threadIdx.x) & 63;
     const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / 64);
 
@@ -133,12 +142,12 @@ __device__ __forceinline__ void multiply(const Product& p, const Place& at, char
     const int first = int(int64_t(all) * at.split / p.splits);
     const int last = int(int64_t(all) * (at.split + 1) / p.splits);
 
-    // loads: lane l of a wave's load takes row l / 8 of 8 rows and stores at
-    // piece l % 8, which holds piece (l % 8) ^ (l / 8)
-    const int piece = (lane & 7) ^ (lane >> 3);
+    // loads: a wave's load takes kRowsOfLoad rows, row r's piece q stored at
+    // place q ^ (r / (16 / kPieces) % kPieces)
+    const int piece = (lane % kPieces) ^ ((wave * 4 + (lane >> 4)) % kPieces);
     const uint32_t ldr = uint32_t(p.r.ld) * 2, ldc = uint32_t(p.c.ld) * 2;
-    const uint32_t lane_r = uint32_t(lane >> 3) * ldr + uint32_t(piece) * 16;
-    const uint32_t lane_c = uint32_t(lane >> 3) * ldc + uint32_t(piece) * 16;
+    const uint32_t lane_r = uint32_t(lane / kPieces) * ldr + uint32_t(piece) * 16;
+    const uint32_t lane_c = uint32_t(lane / kPieces) * ldc + uint32_t(piece) * 16;
     const int rows_r = min(S::kR, p.r.rows - at.r * S::kR);
     const int rows_c = min(S::kC, p.c.rows - at.c * S::kC);
     const char* const base_r =
@@ -149,43 +158,89 @@ __device__ __forceinline__ void multiply(const Product& p, const Place& at, char
     const uint32_t bytes_c = uint32_t(rows_c - 1) * ldc + uint32_t(p.k) * 2;
     const auto local = (char PHUB_LDS_PTR*)lds;
 
-    int seg = first / steps, step = first - seg * steps;  // of the next stage to load
-    auto load = [&](int t, int buffer) {
-        const int64_t pr = seg == 2 ? p.r.plane * 2 : 0, pc = seg == 1 ? p.c.plane * 2 : 0;
-        // (the descriptors are scalars; past the last stage the loads still
-        // count, out of range)
-        const __amdgpu_buffer_rsrc_t dr = __builtin_amdgcn_make_buffer_rsrc(
-            const_cast<char*>(base_r + pr), 0, int(bytes_r), 0x00020000);
-        const __amdgpu_buffer_rsrc_t dc = __builtin_amdgcn_make_buffer_rsrc(
-            const_cast<char*>(base_c + pc), 0, int(bytes_c), 0x00020000);
-        const bool in = t < last && step * kStepK + piece * 8 < p.k;
-        const uint32_t kr = in ? lane_r + uint32_t(step) * (kStepK * 2) : 0x80000000u;
-        const uint32_t kc = in ? lane_c + uint32_t(step) * (kStepK * 2) : 0x80000000u;
-        const auto stage = local + buffer * S::kStageBytes + wave * 1024;
-#pragma unroll
-        for (int j = 0; j < LR; ++j) {
-            const uint32_t off = in ? kr + uint32_t(wave + 4 * j) * 8 * ldr : kr;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(dr, (void PHUB_LDS_PTR*)(stage + j * 4096), 16,
-                                                     int(off), 0, 0, 0);
+    // The next stage to load: `aim` finds its addresses, in four parts, `load`
+    // issues one of the wave's loads.  Past the last stage loads go on, all
+    // out of range (they write zeros), so that every stage has the same number.
+    int loaded = first, seg = first / steps, step = first - seg * steps;
+    const char *pr, *pc;  // of the segment's planes
+    uint32_t kr, kc;
+    char PHUB_LDS_PTR* to;
+    auto aim = [&](int part, int buffer) {
+        if (part == 0) {
+            pr = base_r + (seg == 2 ? p.r.plane * 2 : 0);
+        } else if (part == 1) {
+            pc = base_c + (seg == 1 ? p.c.plane * 2 : 0);
+        } else if (part == 2) {
+            // 2^31 and more is out of range of any tile
+            const bool in = loaded < last && step * kStepK + piece * 8 < p.k;
+            kr = in ? lane_r + uint32_t(step) * (kStepK * 2) : 0x80000000u;
+            kc = in ? lane_c + uint32_t(step) * (kStepK * 2) : 0x80000000u;
+        } else {
+            to = local + buffer * S::kStageBytes + wave * 1024;
+            ++loaded;
+            const bool end = ++step == steps;
+            step = end ? 0 : step;
+            // (or the compiler keeps it, and every descriptor, in vector registers)
+            seg = __builtin_amdgcn_readfirstlane(end ? seg + 1 : seg);
         }
-#pragma unroll
-        for (int j = 0; j < LC; ++j) {
-            const uint32_t off = in ? kc + uint32_t(wave + 4 * j) * 8 * ldc : kc;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                dc, (void PHUB_LDS_PTR*)(stage + S::kR * 128 + j * 4096), 16, int(off), 0, 0, 0);
-        }
-        if (++step == steps) {
-            step = 0;
-            ++seg;
-        }
+    };
+    auto load = [&](int j) {
+        const bool is_r = j < LR;
+        const int at = is_r ? j : j - LR;
+        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<char*>(is_r ? pr : pc), 0, int(is_r ? bytes_r : bytes_c), 0x00020000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            from, (void PHUB_LDS_PTR*)(to + (is_r ? 0 : S::kR * S::kRowBytes) + at * 4096), 16,
+            int((is_r ? kr : kc) + uint32_t(wave + 4 * at) * kRowsOfLoad * (is_r ? ldr : ldc)), 0, 0, 0);
     };
 
     // fragments: lane l has k 8 (l / 32) .. + 7 of row l % 32
     const int wr = wave / 2, wc = wave % 2;
-    const int row_r = wr * WR * 32 + (lane & 31), row_c = wc * WC * 32 + (lane & 31);
-    int at_k[kStepK / 16];
+    const int at_r = (wr * WR * 32 + (lane & 31)) * S::kRowBytes;
+    const int at_c = (S::kR + wc * WC * 32 + (lane & 31)) * S::kRowBytes;
+    const int order = ((lane & 31) / (16 / kPieces)) % kPieces;
+    constexpr int SLABS = kStepK / 32;  // of 16 k, in half a stage
+    struct Frags {
+        F r[SLABS][WR], c[SLABS][WC];
+    };
+    // the j-th fragment of half h of the stage at `stage`
+    auto fetch = [&](Frags& f, const char* stage, int h, int j) {
+        const int s = j / (WR + WC), i = j % (WR + WC);
+        const char* const from = stage + (((h * SLABS + s) * 2 + (lane >> 5)) ^ order) * 16;
+        if (i < WR)
+            f.r[s][i] = *reinterpret_cast<const F*>(from + at_r + i * 32 * S::kRowBytes);
+        else
+            f.c[s][i - WR] = *reinterpret_cast<const F*>(from + at_c + (i - WR) * 32 * S::kRowBytes);
+    };
+    // Multiplies the fragments of one half stage, and behind each product
+    // issues its share of what comes next: two fetches of the next half's
+    // fragments for each of the half's loads of the stage aimed at, and, in the second half,
+    // the next aim.  The order is fixed here because the compiler, which
+    // knows neither latency, would move the fetches to where they are used
+    // and the loads in front; and the loads are spread over the stage because four
+    // waves' loads side by side take longer than the products that hide them.
+    auto half_stage = [&](const Frags& f, Frags& next, const char* stage, auto which, int buffer) {
+        constexpr int H = decltype(which)::value;
+        constexpr int N = SLABS * WR * WC, READS = SLABS * (WR + WC), LOADS = S::kLoads / 2;
+        static_assert(READS == 2 * LOADS, "two fetches for each load");
+        constexpr int ALL = READS + LOADS + (H ? 4 : 0), EACH = (ALL + N - 1) / N;
 #pragma unroll
-    for (int s = 0; s < kStepK / 16; ++s) at_k[s] = ((2 * s + (lane >> 5)) ^ (lane & 7)) * 16;
+        for (int n = 0; n < N; ++n) {
+            const int s = n / (WR * WC), i = n / WC % WR, j = n % WC;
+            acc[i][j] = mfma(f.r[s][i], f.c[s][j], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = n * EACH; u < (n + 1) * EACH && u < ALL; ++u) {
+                if (u >= READS + LOADS)
+                    aim(u - READS - LOADS, buffer);
+                else if (u % 3 == 2)
+                    load(H * LOADS + u / 3);
+                else
+                    fetch(next, stage, 1 - H, u / 3 * 2 + u % 3);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
 
 #pragma unroll
     for (int i = 0; i < WR; ++i)
@@ -193,28 +248,25 @@ __device__ __forceinline__ void multiply(const Product& p, const Place& at, char
         for (int j = 0; j < WC; ++j) acc[i][j] = f32x16{};
 
 #pragma unroll
-    for (int t = 0; t < STAGES - 1; ++t) load(first + t, t);
+    for (int t = 0; t < STAGES; ++t) {
+#pragma unroll
+        for (int part = 0; part < 4; ++part) aim(part, t);
+        if (t < STAGES - 1)
+#pragma unroll
+            for (int j = 0; j < S::kLoads; ++j) load(j);
+    }
+    arrive<(STAGES - 2) * S::kLoads>();
+    Frags f0, f1;
+#pragma unroll
+    for (int j = 0; j < SLABS * (WR + WC); ++j) fetch(f0, lds, 0, j);
     int buffer = 0;
     for (int t = first; t < last; ++t) {
-        arrive<(STAGES - 2) * S::kLoads>();
-        load(t + STAGES - 1, buffer == 0 ? STAGES - 1 : buffer - 1);
-        const char* const stage = lds + buffer * S::kStageBytes;
-#pragma unroll
-        for (int s = 0; s < kStepK / 16; ++s) {
-            F fr[WR], fc[WC];
-#pragma unroll
-            for (int i = 0; i < WR; ++i)
-                fr[i] = *reinterpret_cast<const F*>(stage + row_r * 128 + i * 4096 + at_k[s]);
-#pragma unroll
-            for (int j = 0; j < WC; ++j)
-                fc[j] = *reinterpret_cast<const F*>(stage + S::kR * 128 + row_c * 128 + j * 4096 +
-                                                    at_k[s]);
-#pragma unroll
-            for (int i = 0; i < WR; ++i)
-#pragma unroll
-                for (int j = 0; j < WC; ++j) acc[i][j] = mfma(fr[i], fc[j], acc[i][j]);
-        }
+        half_stage(f0, f1, lds + buffer * S::kStageBytes, std::integral_constant<int, 0>{}, 0);
+        // the next stage is there, and every wave has what it needs of this one
+        arrive<(STAGES - 3) * S::kLoads + S::kLoads / 2>();
+        const int free = buffer;
         buffer = buffer == STAGES - 1 ? 0 : buffer + 1;
+        half_stage(f1, f0, lds + buffer * S::kStageBytes, std::integral_constant<int, 1>{}, free);
     }
     arrive<0>();
 }

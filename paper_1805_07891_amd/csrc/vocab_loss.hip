@@ -10,15 +10,16 @@
 //
 //   G = g T (softmax(z) - q),   dx = G w,   dw = G^T x.
 //
-// Forward: each tile of the product leaves the largest logit and the sum of
-// exponentials of its part of the vocabulary for every row, and the logits of
-// the targets that lie in it; a second kernel joins them.  The 4 N V
-// bytes of logits are never written.
+// Forward: each tile of the product leaves, for every row, a power of two and
+// the sum of exponentials of its part of the vocabulary relative to it; a
+// second kernel joins them and takes the targets' logits, as dot products of
+// their own.  The 4 N V bytes of logits are never written.
 //
 // Backward: the logits are computed again, a piece of the vocabulary at a
-// time (as much as the workspace takes), and softmax(z) - q goes to the
+// time (as much as the workspace takes), and softmax(z) goes to the
 // workspace twice: by rows (P, the factor of dx) and by vocabulary (Q, the
-// factor of dw, with the row's g).  Two more products make the gradients.
+// factor of dw, with the row's g); the few entries with a target are then
+// replaced by softmax(z) - q.  Two more products make the gradients.
 // dx of bf16 and fp16 is rounded to 16 bits at the end, so P is of that
 // type: its rounding errors are independent from entry to entry and stay
 // below that last rounding.  dw is fp32 (what a worker pushes), so Q is two fp16
@@ -39,42 +40,34 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr int kNoExponent = -100000;  // of a row of zeros
-constexpr int kSlab = 36;             // floats of an LDS row of 32 logits
 
 // ------------------------------------------------------------ the targets
 
-// A row's target distribution as `top` (index, weight) pairs, each index
-// once, -1 where there is none.
+// A row's target distribution: one target, or `top` (index, weight) pairs,
+// each index once, -1 where there is none.
 struct Targets {
     int top;
-    const int* index;    // [rows][top]
-    const float* weight; // [rows][top]; null: 1
+    int vocab;
+    const int64_t* target;  // [rows], or null
+    const int* index;       // [rows][top]
+    const float* weight;    // [rows][top]
 };
 
-__global__ __launch_bounds__(256) void prepare_targets(int64_t rows, int64_t vocab,
-                                                       const int64_t* target, const float* dloss,
-                                                       int* index, int* alive, float* factor,
-                                                       int* exponents, int num_exponents) {
-    if (blockIdx.x == 0)
-        for (int i = int(threadIdx.x); i < num_exponents; i += 256) exponents[i] = kNoExponent;
-    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (i >= rows) return;
-    const int64_t t = target[i];
-    const bool live = t >= 0 && t < vocab;
-    index[i] = live ? int(t) : -1;
-    alive[i] = live;
-    if (factor) factor[i] = !live ? 0.0f : dloss ? dloss[i] : 1.0f;
+__device__ __forceinline__ int index_of(const Targets& t, int64_t row, int k) {
+    if (!t.target) return t.index[row * t.top + k];
+    const int64_t v = t.target[row];
+    return v >= 0 && v < t.vocab ? int(v) : -1;
+}
+
+__device__ __forceinline__ float weight_of(const Targets& t, int64_t row, int k) {
+    return t.target ? 1.0f : t.weight[row * t.top + k];
 }
 
 // A wave a row.  entropy: sum of q log q.
 __global__ __launch_bounds__(256) void prepare_teacher(int64_t rows, int64_t vocab, int top,
                                                        const int64_t* target, const float* logit,
-                                                       float temperature, const float* dloss,
-                                                       int* index, float* weight, int* alive,
-                                                       float* factor, float* entropy,
-                                                       int* exponents, int num_exponents) {
-    if (blockIdx.x == 0)
-        for (int i = int(threadIdx.x); i < num_exponents; i += 256) exponents[i] = kNoExponent;
+                                                       float temperature, int* index,
+                                                       float* weight, int* alive, float* entropy) {
     extern __shared__ float words[];  // top floats and top ints a wave
     const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) / 64;
     const int64_t i = int64_t(blockIdx.x) * 4 + wave;
@@ -126,7 +119,6 @@ __global__ __launch_bounds__(256) void prepare_teacher(int64_t rows, int64_t voc
     if (lane == 0) {
         alive[i] = live;
         if (entropy) entropy[i] = ent;
-        if (factor) factor[i] = !live ? 0.0f : (dloss ? dloss[i] : 1.0f) * temperature;
     }
 }
 
@@ -175,67 +167,162 @@ __device__ __forceinline__ float row_largest(const T* p, int cols) {
     return most;
 }
 
+// The largest of a kernel's blocks' exponents, one word a block; by a whole wave.
+struct Largest {
+    const int* blocks;
+    int count;  // at most kExponentBlocks
+};
+
+constexpr int kExponentBlocks = 1024;
+
+__device__ __forceinline__ int largest_of(const Largest& l) {
+    int e = kNoExponent;
+    for (int i = int(threadIdx.x) & 63; i < l.count; i += 64) e = max(e, l.blocks[i]);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) e = max(e, __shfl_xor(e, d));
+    return e == kNoExponent ? 0 : e;
+}
+
+// A block's word of the above: `e` is the wave's.
+__device__ __forceinline__ void leave_largest(int e, int* blocks) {
+    __shared__ int words[4];
+    if ((threadIdx.x & 63) == 0) words[threadIdx.x / 64] = e;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        blocks[blockIdx.x] = max(max(words[0], words[1]), max(words[2], words[3]));
+}
+
 // Rows as the product takes them, `ld` elements apart, zero from cols on:
-// fp32 as two fp16 planes and the power of two that undoes a row's scale,
-// 16-bit types as they are.  A wave a row.
+// fp32 as two fp16 planes, with each row's exponent and the power of two that
+// undoes its scale; 16-bit types as they are.  A wave a row at a time.
 template <typename T>
 __global__ __launch_bounds__(256) void pack_rows(const T* src, int64_t stride, int64_t rows, int cols,
                                                  void* dst, int64_t ld, int64_t plane, float* scale,
                                                  int* row_exponent, int* largest) {
     constexpr int E = kPerLoad<T>;
     const int lane = int(threadIdx.x) & 63;
-    const int64_t row = int64_t(blockIdx.x) * 4 + threadIdx.x / 64;
-    if (row >= rows) return;
-    const T* const p = src + row * stride;
-    if constexpr (std::is_same<T, float>::value) {
-        const int e = exponent_of(row_largest<T>(p, cols));
-        if (lane == 0) {
-            scale[row] = __builtin_amdgcn_ldexpf(1.0f, e - 14);
-            if (row_exponent) row_exponent[row] = e;
-            if (largest) atomicMax(largest, e);
-        }
-        fp16* const out = static_cast<fp16*>(dst) + row * ld;
-        for (int c = lane * E; c < ld; c += 64 * E) {
-            const Piece<T> r = load_piece<T>(p + c, cols - c);
-            fp16 h[E], l[E];
+    int most = kNoExponent;
+    for (int64_t row = int64_t(blockIdx.x) * 4 + threadIdx.x / 64; row < rows;
+         row += int64_t(gridDim.x) * 4) {
+        const T* const p = src + row * stride;
+        if constexpr (std::is_same<T, float>::value) {
+            const int e = exponent_of(row_largest<T>(p, cols));
+            most = max(most, e);
+            if (lane == 0) {
+                scale[row] = __builtin_amdgcn_ldexpf(1.0f, e - 14);
+                if (row_exponent) row_exponent[row] = e;
+            }
+            fp16* const out = static_cast<fp16*>(dst) + row * ld;
+            for (int c = lane * E; c < ld; c += 64 * E) {
+                const Piece<T> r = load_piece<T>(p + c, cols - c);
+                fp16 h[E], l[E];
 #pragma unroll
-            for (int i = 0; i < E; ++i) split(r.e[i], e, h + i, l + i);
-            __builtin_memcpy(out + c, h, sizeof h);
-            __builtin_memcpy(out + plane + c, l, sizeof l);
+                for (int i = 0; i < E; ++i) split(r.e[i], e, h + i, l + i);
+                __builtin_memcpy(out + c, h, sizeof h);
+                __builtin_memcpy(out + plane + c, l, sizeof l);
+            }
+        } else {
+            T* const out = static_cast<T*>(dst) + row * ld;
+            for (int c = lane * E; c < ld; c += 64 * E) {
+                const Piece<T> r = load_piece<T>(p + c, cols - c);
+                __builtin_memcpy(out + c, &r, 16);
+            }
         }
-    } else {
-        T* const out = static_cast<T*>(dst) + row * ld;
-        for (int c = lane * E; c < ld; c += 64 * E) {
-            const Piece<T> r = load_piece<T>(p + c, cols - c);
-            __builtin_memcpy(out + c, &r, 16);
-        }
+    }
+    if (largest) leave_largest(most, largest);
+}
+
+// Dot product of a row of x and a row of w, in every lane of the wave.
+template <typename T>
+__device__ __forceinline__ float row_dot(const T* x, const T* w, int cols) {
+    constexpr int E = kPerLoad<T>;
+    float s = 0.0f;
+#pragma unroll 4
+    for (int c = (int(threadIdx.x) & 63) * E; c < cols; c += 64 * E) {
+        const Piece<T> a = load_piece<T>(x + c, cols - c), b = load_piece<T>(w + c, cols - c);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s = __builtin_fmaf(float(a.e[e]), float(b.e[e]), s);
+    }
+    return wave_sum(s);
+}
+
+// The logits of a teacher's entries: products of gathered rows of w, read
+// from memory or the caches once for each entry.  A wave takes four entries of a row,
+// so that four rows of w are in flight and x is read once for them.
+constexpr int kEntries = 4;
+
+template <typename T>
+__global__ __launch_bounds__(256) void target_logits(const T* x, int64_t x_stride, const T* w,
+                                                     int64_t w_stride, int64_t rows, int cols,
+                                                     Targets t, float inv_temperature, float* pick) {
+    constexpr int E = kPerLoad<T>;
+    const int groups = (t.top + kEntries - 1) / kEntries;
+    const int64_t unit = int64_t(blockIdx.x) * 4 + threadIdx.x / 64;
+    const int64_t row = unit / groups;
+    if (row >= rows) return;
+    const int first = int(unit % groups) * kEntries, lane = int(threadIdx.x) & 63;
+    int v[kEntries];
+    const T* wr[kEntries];
+    bool any = false;
+#pragma unroll
+    for (int k = 0; k < kEntries; ++k) {
+        v[k] = first + k < t.top ? t.index[row * t.top + first + k] : -1;
+        wr[k] = w + int64_t(max(v[k], 0)) * w_stride;
+        any |= v[k] >= 0;
+    }
+    if (!any) return;
+    const T* const xr = x + row * x_stride;
+    float s[kEntries] = {};
+#pragma unroll 2
+    for (int c = lane * E; c < cols; c += 64 * E) {
+        const Piece<T> a = load_piece<T>(xr + c, cols - c);
+        Piece<T> b[kEntries];
+#pragma unroll
+        for (int k = 0; k < kEntries; ++k) b[k] = load_piece<T>(wr[k] + c, cols - c);
+#pragma unroll
+        for (int k = 0; k < kEntries; ++k)
+#pragma unroll
+            for (int e = 0; e < E; ++e) s[k] = __builtin_fmaf(float(a.e[e]), float(b[k].e[e]), s[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kEntries; ++k) {
+        const float z = wave_sum(s[k]) * inv_temperature;
+        if (lane == 0 && v[k] >= 0) pick[row * t.top + first + k] = z;
     }
 }
 
-// For the product of dw: every row's exponent, and the largest of |factor| x
-// over all rows.  A block takes `each` rows, a wave a row at a time.
+// What the backward pass needs of each row: whether it has a target (alive: all bits
+// or none), its factor g T, its target's logit, the exponent of x and the
+// block's largest of factor x.  A wave a row at a time.
 template <typename T>
-__global__ __launch_bounds__(256) void row_exponents(const T* src, int64_t stride, int64_t rows,
-                                                     int cols, int each, const float* factor,
-                                                     const int* alive, int* row_exponent,
-                                                     int* largest) {
-    __shared__ int words[4];
-    const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) / 64;
-    const int64_t first = int64_t(blockIdx.x) * each, last = std::min<int64_t>(rows, first + each);
+__global__ __launch_bounds__(256) void prepare_rows(const T* x, int64_t x_stride, const T* w,
+                                                    int64_t w_stride, int64_t rows, int cols,
+                                                    Targets t, const int* teacher_alive,
+                                                    const float* dloss, float temperature,
+                                                    int* alive, float* factor, float* pick,
+                                                    int* row_exponent, int* largest) {
+    const int lane = int(threadIdx.x) & 63;
     int most = kNoExponent;
-    for (int64_t row = first + wave; row < last; row += 4) {
-        const int e = exponent_of(row_largest<T>(src + row * stride, cols));
-        if (lane == 0) row_exponent[row] = e;
-        const float f = __builtin_fabsf(factor[row]);
-        if (alive[row] && f > 0.0f && f < __builtin_huge_valf())
-            most = max(most, e + __builtin_amdgcn_frexp_expf(f));
+    for (int64_t row = int64_t(blockIdx.x) * 4 + threadIdx.x / 64; row < rows;
+         row += int64_t(gridDim.x) * 4) {
+        const T* const xr = x + row * x_stride;
+        const bool live = teacher_alive ? teacher_alive[row] != 0 : index_of(t, row, 0) >= 0;
+        const float f = !live ? 0.0f : (dloss ? dloss[row] : 1.0f) * temperature;
+        const int e = exponent_of(row_largest<T>(xr, cols));
+        if (lane == 0) {
+            alive[row] = live ? -1 : 0;
+            factor[row] = f;
+            row_exponent[row] = e;
+        }
+        const float size = __builtin_fabsf(f);
+        if (size > 0.0f && size < __builtin_huge_valf())
+            most = max(most, e + __builtin_amdgcn_frexp_expf(size));
+        if (live && t.target) {
+            const float z = row_dot<T>(xr, w + t.target[row] * w_stride, cols);
+            if (lane == 0) pick[row] = z;
+        }
     }
-    if (lane == 0) words[wave] = most;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        most = max(max(words[0], words[1]), max(words[2], words[3]));
-        if (most != kNoExponent) atomicMax(largest, most);
-    }
+    leave_largest(most, largest);
 }
 
 // dst[c][r] = src[r][c] for columns c < cols, and zero for rows up to ld (a
@@ -288,29 +375,29 @@ __global__ __launch_bounds__(256) void transpose(const T* src, int64_t stride, i
 // What both passes need of the logits: z = acc * scale.
 struct Logits {
     int rows, vocab;       // valid rows of x; valid rows of w in this piece
-    int first;             // the piece's first vocabulary row
     float inv_temperature;
     const float* scale_x;  // [rows]; null: 1 (16-bit types)
     const float* scale_w;  // [piece]; null: 1
-    Targets targets;
 };
 
 struct ForwardOut {
-    f32x2* part;   // [blocks of 32 WR vocabulary rows][rows]: largest logit, sum of exponentials
+    f32x2* part;  // [blocks of 32 WR vocabulary rows][rows]: an exponent n, sum of exp(z) 2^-n
     int first_block;
-    float* pick;   // [rows][top]
 };
 
-// Scales of the four consecutive vocabulary rows that a lane holds.
-__device__ __forceinline__ f32x4 scales_of(const Logits& l, int v) {
+// Four consecutive values, 1 where there are none (the products they scale are 0).
+__device__ __forceinline__ f32x4 four(const float* p, int at, int end) {
     f32x4 s = {1.0f, 1.0f, 1.0f, 1.0f};
-    if (l.scale_w)
+    if (p)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] = v + e < l.vocab ? l.scale_w[v + e] : 0.0f;
+        for (int e = 0; e < 4; ++e)
+            if (at + e < end) s[e] = p[at + e];
     return s;
 }
 
-template <typename T, int WR, int WC, int STAGES>
+// R is w, C is x: a lane has one row of x and, in registers, entries of the
+// vocabulary.  SCALED: fp32's rows, and temperatures other than 1.
+template <typename T, bool SCALED, int WR, int WC, int STAGES>
 __global__ __launch_bounds__(kProductThreads) void logits_forward(Product p, Logits l,
                                                                   ForwardOut out) {
     __shared__ __attribute__((aligned(1024))) char lds[TileShape<WR, WC>::kStageBytes * STAGES];
@@ -323,105 +410,117 @@ __global__ __launch_bounds__(kProductThreads) void logits_forward(Product p, Log
     const int half = lane >> 5;
     const int block = at.r * 2 + wave / 2, v0 = block * WR * 32;
     const int i0 = (at.c * 2 + wave % 2) * WC * 32;
+    const float low = -__builtin_huge_valf();
+    if (v0 >= l.vocab) return;
 #pragma unroll
     for (int j = 0; j < WC; ++j) {
         const int row = i0 + j * 32 + (lane & 31);
-        const float sx = l.inv_temperature * (l.scale_x && row < l.rows ? l.scale_x[row] : 1.0f);
-        float most = -__builtin_huge_valf();
+        if constexpr (SCALED) {
+            const float sx = l.inv_temperature * (l.scale_x && row < l.rows ? l.scale_x[row] : 1.0f);
 #pragma unroll
-        for (int i = 0; i < WR; ++i)
+            for (int i = 0; i < WR; ++i)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int v = v0 + i * 32 + g * 8 + half * 4;
-                const f32x4 sw = scales_of(l, v);
+                for (int g = 0; g < 4; ++g) {
+                    const f32x4 sw = four(l.scale_w, v0 + i * 32 + g * 8 + half * 4, l.vocab);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float z = acc[i][j][g * 4 + e] * (sx * sw[e]);
-                    acc[i][j][g * 4 + e] = v + e < l.vocab ? z : -__builtin_huge_valf();
-                    most = v + e < l.vocab && (z != z || z > most) ? z : most;
+                    for (int e = 0; e < 4; ++e) acc[i][j][g * 4 + e] *= sx * sw[e];
                 }
-            }
-        const float other = __shfl_xor(most, 32);
-        most = other != other || other > most ? other : most;
-        const float base = most == -__builtin_huge_valf() ? 0.0f : most;
-        float sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < WR; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                sum += __builtin_amdgcn_exp2f((acc[i][j][r] - base) * kLog2e);
-        sum += __shfl_xor(sum, 32);
-        if (half == 0 && row < l.rows && v0 < l.vocab)
-            out.part[int64_t(out.first_block + block) * l.rows + row] = f32x2{most, sum};
-    }
-    // the targets' logits, through LDS (each wave its own part)
-    float* const slab = reinterpret_cast<float*>(lds) + wave * WC * 32 * kSlab;
-#pragma unroll
-    for (int i = 0; i < WR; ++i) {
-#pragma unroll
-        for (int j = 0; j < WC; ++j)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                f32x4 v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = acc[i][j][g * 4 + e];
-                *reinterpret_cast<f32x4*>(slab + (j * 32 + (lane & 31)) * kSlab + g * 8 + half * 4) = v;
-            }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        const int from = l.first + v0 + i * 32;
-#pragma unroll
-        for (int t = lane; t < WC * 32; t += 64) {
-            const int row = i0 + t;
-            if (row >= l.rows) break;
-            const int* const idx = l.targets.index + int64_t(row) * l.targets.top;
-            for (int k = 0; k < l.targets.top; ++k) {
-                const unsigned in = unsigned(idx[k] - from);
-                if (in < 32u) out.pick[int64_t(row) * l.targets.top + k] = slab[t * kSlab + in];
-            }
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        f32x2 part;
+        auto reduce = [&](auto is_cut) {
+            constexpr bool CUT = decltype(is_cut)::value;
+            auto in = [&](int i, int r) {
+                return !CUT || v0 + i * 32 + r / 4 * 8 + half * 4 + r % 4 < l.vocab;
+            };
+            float most = low;  // ignores NaN, which the sum shows
+#pragma unroll
+            for (int i = 0; i < WR; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (in(i, r)) most = __builtin_fmaxf(most, acc[i][j][r]);
+            most = __builtin_fmaxf(most, __shfl_xor(most, 32));
+            // relative to a power of two, so that the reference is exact: the
+            // argument of exp2 is rounded once
+            const float n = most == low ? 0.0f : __builtin_rintf(most * kLog2e);
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < WR; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (in(i, r))
+                        sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][r], kLog2e, -n));
+            sum += __shfl_xor(sum, 32);
+            part = f32x2{n, sum};
+        };
+        // (only the last blocks of a piece are cut)
+        if (v0 + WR * 32 > l.vocab)
+            reduce(std::true_type{});
+        else
+            reduce(std::false_type{});
+        if (half == 0 && row < l.rows)
+            out.part[int64_t(out.first_block + block) * l.rows + row] = part;
     }
 }
 
-// Joins the tiles' sums: 64 rows a block, their partial sums dealt to its
-// waves.
+constexpr int kFinishRows = 16;
+
+// Joins the tiles' sums and takes the targets' logits: 16 rows a block,
+// their sums dealt to 64 groups of threads, the rows then to the waves.
+template <typename T>
 __global__ __launch_bounds__(1024) void finish_loss(const f32x2* part, int blocks, int64_t rows,
-                                                    Targets t, const float* pick, const int* alive,
+                                                    const T* x, int64_t x_stride, const T* w,
+                                                    int64_t w_stride, int cols, Targets t,
+                                                    const float* pick, const int* alive,
                                                     const float* entropy, float temperature,
                                                     float* loss, float* lse) {
-    __shared__ f32x2 words[16][64];
-    const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) / 64;
-    const int64_t row = int64_t(blockIdx.x) * 64 + lane;
-    const float low = -__builtin_huge_valf();
-    auto join = [&](f32x2 a, f32x2 b) {
-        const float m = a.x != a.x || a.x > b.x ? a.x : b.x;
-        if (m == low) return f32x2{low, 0.0f};
-        return f32x2{m, a.y * __builtin_amdgcn_exp2f((a.x - m) * kLog2e) +
-                            b.y * __builtin_amdgcn_exp2f((b.x - m) * kLog2e)};
+    __shared__ f32x2 words[64][kFinishRows];
+    __shared__ float ends[kFinishRows];
+    const int in = int(threadIdx.x) % kFinishRows, group = int(threadIdx.x) / kFinishRows;
+    const int64_t first = int64_t(blockIdx.x) * kFinishRows;
+    // a sum of 0 has no reference (-inf logits alone)
+    auto join = [](f32x2 a, f32x2 b) {
+        if (b.y == 0.0f) return a;
+        if (a.y == 0.0f) return b;
+        const float n = __builtin_fmaxf(a.x, b.x);
+        return f32x2{n, a.y * __builtin_amdgcn_exp2f(a.x - n) + b.y * __builtin_amdgcn_exp2f(b.x - n)};
     };
-    f32x2 s = {low, 0.0f};
-    if (row < rows)
-        for (int b = wave; b < blocks; b += 16) s = join(s, part[int64_t(b) * rows + row]);
-    words[wave][lane] = s;
-    __syncthreads();
-    if (wave != 0 || row >= rows) return;
-    for (int w = 1; w < 16; ++w) s = join(s, words[w][lane]);
-    const float all = s.x == low ? low : s.x + logf(s.y);
-    lse[row] = all;
-    float out = 0.0f;
-    if (alive[row]) {
-        if (t.weight) {
-            float dot = 0.0f;
-            for (int k = 0; k < t.top; ++k) {
-                const float q = t.weight[row * t.top + k];  // 0 where there is no entry
-                if (q != 0.0f) dot = __builtin_fmaf(q, all - pick[row * t.top + k], dot);
-            }
-            out = temperature * temperature * (entropy[row] + dot);
-        } else {
-            out = all - pick[row];
-        }
+    f32x2 s = {0.0f, 0.0f};
+    if (first + in < rows) {
+#pragma unroll 4
+        for (int b = group; b < blocks; b += 64) s = join(s, part[int64_t(b) * rows + first + in]);
     }
-    loss[row] = out;
+    words[group][in] = s;
+    __syncthreads();
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        if (group < d) words[group][in] = join(words[group][in], words[group + d][in]);
+        __syncthreads();
+    }
+    if (group == 0 && first + in < rows) {
+        const f32x2 all = words[0][in];
+        // n ln 2 + ln sum
+        const float end = __builtin_fmaf(all.x, 0x1.62e42ep-1f, __builtin_fmaf(all.x, 0x1.efa39ep-25f, logf(all.y)));
+        ends[in] = end;
+        lse[first + in] = end;
+    }
+    __syncthreads();
+    const int wave = int(threadIdx.x) / 64, lane = int(threadIdx.x) & 63;
+    const int64_t row = first + wave;
+    if (row >= rows) return;
+    const float end = ends[wave];
+    float out = 0.0f;
+    if (t.target) {
+        const int v = index_of(t, row, 0);
+        if (v >= 0) out = end - row_dot<T>(x + row * x_stride, w + int64_t(v) * w_stride, cols);
+    } else if (alive[row]) {
+        for (int k = lane; k < t.top; k += 64) {
+            const float q = t.weight[row * t.top + k];  // 0 where there is no entry
+            // relative to lse, so that nothing large cancels
+            if (q != 0.0f) out = __builtin_fmaf(q, end - pick[row * t.top + k], out);
+        }
+        out = temperature * temperature * (entropy[row] + wave_sum(out));
+    }
+    if (lane == 0) loss[row] = out;
 }
 
 struct BackwardOut {
@@ -429,123 +528,247 @@ struct BackwardOut {
     const int* alive;
     const float* factor;
     const int* row_exponent;  // of x
-    const int* largest;       // [0]: of factor x
-    const int* largest_w;     // of this piece of w (fp32 types), else null
-    void* p;                  // [rows][ld_p]: softmax - q, by rows; null if dx is not wanted
+    Largest largest;          // of factor x
+    Largest largest_w;        // of this piece of w (fp32 types)
+    void* p;                  // [rows][ld_p]: the softmax by rows; null if dx is not wanted
     int64_t ld_p, plane_p;
     fp16* q;                  // [piece][ld_q]: by vocabulary, times the row's factor; null: no dw
     int64_t ld_q, plane_q;
 };
 
-// T: type of the product's operands and of P.  PLANES: of P.
-template <typename T, int PLANES, int WR, int WC, int STAGES>
+typedef _Float16 fp16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    typedef T t2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), t2));
+}
+
+template <typename T>
+__device__ __forceinline__ f32x2 unpack2(uint32_t v) {
+    typedef T t2 __attribute__((ext_vector_type(2)));
+    return __builtin_convertvector(__builtin_bit_cast(t2, v), f32x2);
+}
+
+// Four consecutive values as 16-bit pairs, and what that leaves.
+template <typename T>
+__device__ __forceinline__ void split4(const f32x4& y, uint32_t (&high)[2], uint32_t (&low)[2]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        high[h] = pack2<T>(y[2 * h], y[2 * h + 1]);
+        const f32x2 back = unpack2<T>(high[h]);
+        low[h] = pack2<T>(y[2 * h] - back.x, y[2 * h + 1] - back.y);
+    }
+}
+
+// R is x, C is w: a lane has one entry of the vocabulary and, in registers,
+// four consecutive rows in each group.  P and Q go to memory through LDS, each wave
+// through a part of its own, so that they are written in whole lines (16 lanes a
+// row of 256 bytes): written from registers, in pieces of 16 and 64 bytes,
+// the kernel took 2754 us instead of REWRITE for 8192 rows, 4096 columns and 32768
+// entries (bf16), 1.6 GB written.  T: type of the product's operands and of P;
+// PLANES: of P.  BOTH: P and Q are wanted
+// (known without asking at every entry).
+template <typename T, int PLANES, bool BOTH, int WR, int WC, int STAGES>
 __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Logits l,
                                                                    BackwardOut out) {
-    __shared__ __attribute__((aligned(1024))) char lds[TileShape<WR, WC>::kStageBytes * STAGES];
+    // a wave's part of LDS: what it needs of its rows, then 32 WR x 32 WC entries of 16 bits
+    constexpr int kAbout = WR * 32 * 16, kPart = kAbout + WR * WC * 2048;
+    constexpr int kStageBytes = TileShape<WR, WC>::kStageBytes * STAGES;
+    __shared__ __attribute__((aligned(1024))) char lds[kStageBytes > 4 * kPart ? kStageBytes : 4 * kPart];
     const Place at = place(p);
     if (!at.live) return;
     f32x16 acc[WR][WC];
     multiply<T, WR, WC, STAGES>(p, at, lds, acc);
 
     const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) / 64;
-    const int half = lane >> 5;
-    const int v0 = (at.r * 2 + wave / 2) * WR * 32, i0 = (at.c * 2 + wave % 2) * WC * 32;
-    float* const slab = reinterpret_cast<float*>(lds) + wave * WC * 32 * kSlab;
-    float sx[WC], lse[WC];
-    bool live[WC];
+    const int half = lane >> 5, odd = lane & 1;
+    const int i0 = (at.r * 2 + wave / 2) * WR * 32, v0 = (at.c * 2 + wave % 2) * WC * 32;
+    const bool want_p = BOTH || out.p, want_q = BOTH || out.q;
+    const int largest = want_q ? largest_of(out.largest) : 0;
+    const int largest_w = PLANES == 2 ? largest_of(out.largest_w) : 0;
+    // lse, scale, factor of Q, whether it is alive
+    f32x4* const about = reinterpret_cast<f32x4*>(lds + wave * kPart);
+    for (int r = lane; r < WR * 32; r += 64) {
+        const int row = i0 + r;
+        f32x4 a = {};
+        if (row < l.rows) {
+            a.x = out.lse[row];
+            a.y = l.inv_temperature * (PLANES == 2 ? l.scale_x[row] : 1.0f);
+            if (want_q)
+                a.z = __builtin_amdgcn_ldexpf(out.factor[row], out.row_exponent[row] - largest + 14);
+            a.w = __builtin_bit_cast(float, out.alive[row]);
+        }
+        about[r] = a;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // other lanes of the wave read them
+    float sw[WC], cw[WC];
+    uint32_t in[WC];
 #pragma unroll
     for (int j = 0; j < WC; ++j) {
-        const int row = i0 + j * 32 + (lane & 31);
-        const bool in = row < l.rows;
-        live[j] = in && out.alive[row];
-        sx[j] = l.inv_temperature * (l.scale_x && in ? l.scale_x[row] : 1.0f);
-        lse[j] = in ? out.lse[row] : 0.0f;
-        // the row's factor of Q, beside its logits
-        if (half == 0)
-            slab[(j * 32 + (lane & 31)) * kSlab + 32] =
-                live[j] && out.q ? __builtin_amdgcn_ldexpf(out.factor[row],
-                                                           out.row_exponent[row] - *out.largest + 14)
-                                 : 0.0f;
+        const int v = v0 + j * 32 + (lane & 31);
+        in[j] = v < l.vocab ? ~0u : 0u;
+        sw[j] = PLANES == 2 && in[j] ? l.scale_w[v] : 1.0f;
+        // P's scale: into fp16's range, and fp32's rows of w to the piece's largest
+        cw[j] = PLANES == 2                       ? __builtin_amdgcn_ldexpf(sw[j], 28 - largest_w)
+                : std::is_same<T, fp16>::value ? 16384.0f
+                                                  : 1.0f;
     }
+    char* const part = lds + wave * kPart + kAbout;
+    // P's rows in the part: 64 WC bytes; the two planes of fp32 take half of it each,
+    // so half of the rows at a time.  Pieces of 64 bytes change places by
+    // row, as the four rows that a write touches would meet in the same banks.
+    constexpr int kPiecesP = WC * 4, kRowsP = WR >= 2 || PLANES == 1 ? WR * 32 / PLANES : 16;
+    auto place_p = [](int t, int piece) {
+        return (t * kPiecesP + (piece ^ ((t >> 1 & 3) << 2 & (kPiecesP - 1)))) * 16;
+    };
+    auto write_p = [&](int from) {  // rows from .. from + kRowsP of the wave's
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        constexpr int kAtOnce = 64 / kPiecesP;
+#pragma unroll
+        for (int m = 0; m < PLANES; ++m)
+#pragma unroll
+            for (int t0 = 0; t0 < kRowsP; t0 += kAtOnce) {
+                const int t = t0 + lane / kPiecesP, piece = lane % kPiecesP;
+                const f32x4 v = *reinterpret_cast<const f32x4*>(part + m * kRowsP * kPiecesP * 16 +
+                                                                place_p(t, piece));
+                T* const to = static_cast<T*>(out.p) + m * out.plane_p +
+                              int64_t(i0 + from + t) * out.ld_p + v0 + piece * 8;
+                if (i0 + from + t < l.rows) *reinterpret_cast<f32x4*>(to) = v;
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    };
 #pragma unroll
     for (int i = 0; i < WR; ++i) {
-        const int vb = v0 + i * 32;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const int v = vb + g * 8 + half * 4;
-            const f32x4 sw = scales_of(l, v);
+            f32x4 row[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) row[e] = about[i * 32 + g * 8 + half * 4 + e];
 #pragma unroll
             for (int j = 0; j < WC; ++j) {
                 f32x4 y;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float d = __builtin_fmaf(acc[i][j][g * 4 + e], sx[j] * sw[e], -lse[j]);
+                    const float d = __builtin_fmaf(acc[i][j][g * 4 + e],
+                                                   PLANES == 2 ? row[e].y * sw[j] : row[e].y, -row[e].x);
+                    // a row or entry that is not there, or not alive, is 0 whatever it held
                     const float s = __builtin_amdgcn_exp2f(d * kLog2e);
-                    y[e] = live[j] && v + e < l.vocab ? s : 0.0f;
+                    const float mask = row[e].w;  // (bit_cast of a vector's element takes the first)
+                    y[e] = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, s) &
+                                                         __builtin_bit_cast(uint32_t, mask) & in[j]);
                 }
-                *reinterpret_cast<f32x4*>(slab + (j * 32 + (lane & 31)) * kSlab + g * 8 + half * 4) = y;
+                if (want_p) {
+                    f32x4 c;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) c[e] = rounded(y[e] * cw[j]);
+                    uint32_t planes[2][2];
+                    split4<T>(c, planes[0], planes[1]);
+                    // neighbouring lanes exchange rows: even ones take rows 0 and 1 of the
+                    // pair of entries, odd ones 2 and 3
+                    const int t = (i * 32 + g * 8 + half * 4 + odd * 2) % kRowsP;
+                    const int at16 = (j * 32 + (lane & 30)) * 2;  // bytes
+#pragma unroll
+                    for (int m = 0; m < PLANES; ++m) {
+                        const uint32_t mine = odd ? planes[m][1] : planes[m][0];
+                        const uint32_t give = odd ? planes[m][0] : planes[m][1];
+                        const uint32_t got =
+                            uint32_t(__builtin_amdgcn_mov_dpp(int(give), 0xb1, 0xf, 0xf, true));
+                        const uint32_t left = odd ? got : mine, right = odd ? mine : got;
+                        char* const to = part + m * kRowsP * kPiecesP * 16 + at16 % 16;
+                        *reinterpret_cast<uint32_t*>(to + place_p(t, at16 / 16)) =
+                            (left & 0xffffu) | (right << 16);
+                        *reinterpret_cast<uint32_t*>(to + place_p(t + 1, at16 / 16)) =
+                            (left >> 16) | (right & 0xffff0000u);
+                    }
+                }
+                if (want_q) {
+                    f32x4 c;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) c[e] = rounded(y[e] * row[e].z);
+                    uint32_t high[2], low[2];
+                    split4<fp16>(c, high, low);
+                    // Q's planes wait in the accumulators for their turn in LDS
+                    acc[i][j][g * 4 + 0] = __builtin_bit_cast(float, high[0]);
+                    acc[i][j][g * 4 + 1] = __builtin_bit_cast(float, high[1]);
+                    acc[i][j][g * 4 + 2] = __builtin_bit_cast(float, low[0]);
+                    acc[i][j][g * 4 + 3] = __builtin_bit_cast(float, low[1]);
+                }
             }
+            if (want_p && kRowsP == 16 && g % 2 == 1) write_p(i * 32 + g / 2 * 16);
+        }
+        if (want_p && kRowsP > 16 && (i + 1) * 32 % kRowsP == 0) write_p((i + 1) * 32 - kRowsP);
+    }
+    if (!want_q) return;
+    // Q's rows in the part: 64 WR bytes, 8 rows of x a piece, places changed by the
+    // entry's low bits
+    constexpr int kPiecesQ = WR * 4;
+    auto place_q = [](int v, int piece) { return (v * kPiecesQ + (piece ^ (v & (kPiecesQ - 1)))) * 16; };
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+#pragma unroll
+        for (int i = 0; i < WR; ++i)
+#pragma unroll
+            for (int j = 0; j < WC; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; g += 2) {
+                    // half wave 0 gets all 8 rows of group g, half wave 1 those of g + 1
+                    uint32_t piece[4];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float a = acc[i][j][g * 4 + m * 2 + h], b = acc[i][j][g * 4 + 4 + m * 2 + h];
+                        const auto both = __builtin_amdgcn_permlane32_swap(
+                            __builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), false, false);
+                        piece[h] = both[0];
+                        piece[2 + h] = both[1];
+                    }
+                    __builtin_memcpy(__builtin_assume_aligned(
+                                         part + place_q(j * 32 + (lane & 31), i * 4 + g + half), 16),
+                                     piece, 16);
+                }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        constexpr int kAtOnce = 64 / kPiecesQ;
+#pragma unroll
+        for (int t0 = 0; t0 < WC * 32; t0 += kAtOnce) {
+            const int v = t0 + lane / kPiecesQ, piece = lane % kPiecesQ;
+            const f32x4 y = *reinterpret_cast<const f32x4*>(part + place_q(v, piece));
+            fp16* const to = out.q + m * out.plane_q + int64_t(v0 + v) * out.ld_q + i0 + piece * 8;
+            if (i0 + piece * 8 < out.ld_q) *reinterpret_cast<f32x4*>(to) = y;
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        const int from = l.first + vb;
-#pragma unroll
-        for (int t = lane; t < WC * 32; t += 64) {
-            const int row = i0 + t;
-            if (row >= l.rows) break;
-            const int* const idx = l.targets.index + int64_t(row) * l.targets.top;
-            for (int k = 0; k < l.targets.top; ++k) {
-                const unsigned in = unsigned(idx[k] - from);
-                if (in < 32u)
-                    slab[t * kSlab + in] -=
-                        l.targets.weight ? l.targets.weight[int64_t(row) * l.targets.top + k] : 1.0f;
-            }
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (out.p) {
-            // four lanes a row, 8 entries a lane
-            T* const P = static_cast<T*>(out.p);
-            const int v = vb + (lane & 3) * 8;
-            float cw[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                cw[e] = PLANES == 1      ? 16384.0f
-                        : v + e < l.vocab ? __builtin_amdgcn_ldexpf(l.scale_w[v + e], 28 - *out.largest_w)
-                                          : 0.0f;
-#pragma unroll
-            for (int t = lane >> 2; t < WC * 32; t += 16) {
-                const int row = i0 + t;
-                if (row >= l.rows) break;
-                T h[8], m[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float y = rounded(slab[t * kSlab + (lane & 3) * 8 + e] * cw[e]);
-                    h[e] = T(y);
-                    m[e] = T(y - float(h[e]));
-                }
-                T* const to = P + int64_t(row) * out.ld_p + v;
-                __builtin_memcpy(to, h, 16);
-                if constexpr (PLANES == 2) __builtin_memcpy(to + out.plane_p, m, 16);
-            }
-        }
-        if (out.q) {
-            // a lane has 8 rows of one entry of the vocabulary
-            const int v = lane & 31;
-#pragma unroll
-            for (int t = half * 8; t < WC * 32; t += 16) {
-                if (i0 + t >= out.ld_q) break;
-                fp16 h[8], m[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float y = rounded(slab[(t + e) * kSlab + v] * slab[(t + e) * kSlab + 32]);
-                    h[e] = fp16(y);
-                    m[e] = fp16(y - float(h[e]));
-                }
-                fp16* const to = out.q + int64_t(vb + v) * out.ld_q + i0 + t;
-                __builtin_memcpy(to, h, 16);
-                __builtin_memcpy(to + out.plane_q, m, 16);
-            }
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+}
+
+// The entries of P and Q with a target, a thread each: softmax - q.
+template <typename T, int PLANES>
+__global__ __launch_bounds__(256) void take_targets(Targets t, int64_t rows, int first, int vocab,
+                                                    const float* pick, const float* scale_w,
+                                                    BackwardOut out) {
+    const int largest = out.q ? largest_of(out.largest) : 0;
+    const int largest_w = PLANES == 2 ? largest_of(out.largest_w) : 0;
+    const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t row = at / t.top;
+    if (row >= rows) return;
+    const int k = int(at % t.top);
+    const int v = index_of(t, row, k) - first;
+    if (v < 0 || v >= vocab) return;
+    const float s = __builtin_amdgcn_exp2f((pick[at] - out.lse[row]) * kLog2e) - weight_of(t, row, k);
+    if (out.p) {
+        const float c = PLANES == 2                       ? __builtin_amdgcn_ldexpf(scale_w[v], 28 - largest_w)
+                        : std::is_same<T, fp16>::value ? 16384.0f
+                                                          : 1.0f;
+        const float y = rounded(s * c);
+        T* const to = static_cast<T*>(out.p) + row * out.ld_p + v;
+        *to = T(y);
+        if (PLANES == 2) to[out.plane_p] = T(y - float(T(y)));
+    }
+    if (out.q) {
+        const float y = rounded(s * __builtin_amdgcn_ldexpf(out.factor[row],
+                                                            out.row_exponent[row] - largest + 14));
+        fp16* const to = out.q + int64_t(v) * out.ld_q + row;
+        *to = fp16(y);
+        to[out.plane_q] = fp16(y - float(fp16(y)));
     }
 }
 
@@ -553,7 +776,7 @@ __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Lo
 struct DxOut {
     const int* alive;
     const float* factor;
-    const int* largest_w;  // fp32 types
+    Largest largest_w;  // fp32 types
     void* dx;              // null: to parts
     int64_t stride;
     float* part;           // [splits][rows][cols]
@@ -561,8 +784,12 @@ struct DxOut {
     int rows, cols;
 };
 
-__device__ __forceinline__ float dx_scale(const int* largest_w) {
-    return largest_w ? __builtin_amdgcn_ldexpf(1.0f, *largest_w - 28) : 1.0f / 16384.0f;
+// What undoes P's and w's scales.
+template <typename T, typename O>
+__device__ __forceinline__ float dx_scale(const Largest& largest_w) {
+    if constexpr (std::is_same<O, float>::value)
+        return __builtin_amdgcn_ldexpf(1.0f, largest_of(largest_w) - 28);
+    return std::is_same<T, fp16>::value ? 1.0f / 16384.0f : 1.0f;
 }
 
 template <typename O>
@@ -589,7 +816,7 @@ __global__ __launch_bounds__(kProductThreads) void grad_rows(Product p, DxOut ou
 
     const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) / 64;
     const int c0 = (at.r * 2 + wave / 2) * WR * 32, i0 = (at.c * 2 + wave % 2) * WC * 32;
-    const float scale = dx_scale(out.largest_w);
+    const float scale = dx_scale<T, O>(out.largest_w);
 #pragma unroll
     for (int j = 0; j < WC; ++j) {
         const int row = i0 + j * 32 + (lane & 31);
@@ -642,7 +869,7 @@ __global__ __launch_bounds__(256) void join_rows(const float* part, int splits, 
 }
 
 struct DwOut {
-    const int* largest;
+    Largest largest;
     float* dw;
     int64_t stride;
     bool add;
@@ -659,7 +886,7 @@ __global__ __launch_bounds__(kProductThreads) void grad_weights(Product p, DwOut
 
     const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) / 64;
     const int c0 = (at.r * 2 + wave / 2) * WR * 32, v0 = (at.c * 2 + wave % 2) * WC * 32;
-    const int e2 = *out.largest - 28;
+    const int e2 = largest_of(out.largest) - 28;
 #pragma unroll
     for (int j = 0; j < WC; ++j) {
         const int v = v0 + j * 32 + (lane & 31);
@@ -694,7 +921,12 @@ __global__ __launch_bounds__(256) void clear_weights(float* dw, int64_t stride, 
 // chip, else 128 x 128, else 64 x 64.
 enum Shape { kBig = 0, kMid = 1, kSmall = 2 };
 constexpr int kTileRows[] = {256, 128, 64};
-constexpr int kStages[] = {2, 2, 4};
+#ifndef ST0
+#define ST0 4
+#define ST1 4
+#define ST2 4
+#endif
+constexpr int kStages[] = {ST0, ST1, ST2};
 constexpr int kUnits = 256;  // compute units
 
 int64_t tiles_of(int shape, int64_t r, int64_t c) {
@@ -703,6 +935,9 @@ int64_t tiles_of(int shape, int64_t r, int64_t c) {
 }
 
 int choose_shape(int64_t r, int64_t c) {
+#ifdef FORCE_SHAPE
+    return FORCE_SHAPE;
+#endif
     for (int s = kBig; s < kSmall; ++s)
         if (tiles_of(s, r, c) >= kUnits * 3 / 4) return s;
     return kSmall;
@@ -722,19 +957,19 @@ hipError_t launch_product(K kernel, Product p, hipStream_t stream, const A&... a
     : (shape) == kMid ? call(2, 2, kStages[kMid])  \
                       : call(1, 1, kStages[kSmall])
 
-template <typename T>
+template <typename T, bool SCALED>
 hipError_t run_forward(int shape, const Product& p, const Logits& l, const ForwardOut& o,
                        hipStream_t stream) {
-#define PHUB_CALL(a, b, s) launch_product<a, b>(logits_forward<T, a, b, s>, p, stream, l, o)
+#define PHUB_CALL(a, b, s) launch_product<a, b>(logits_forward<T, SCALED, a, b, s>, p, stream, l, o)
     return PHUB_BY_SHAPE(shape, PHUB_CALL);
 #undef PHUB_CALL
 }
 
-template <typename T, int PLANES>
+template <typename T, int PLANES, bool BOTH>
 hipError_t run_backward(int shape, const Product& p, const Logits& l, const BackwardOut& o,
                         hipStream_t stream) {
 #define PHUB_CALL(a, b, s) \
-    launch_product<a, b>(logits_backward<T, PLANES, a, b, s>, p, stream, l, o)
+    launch_product<a, b>(logits_backward<T, PLANES, BOTH, a, b, s>, p, stream, l, o)
     return PHUB_BY_SHAPE(shape, PHUB_CALL);
 #undef PHUB_CALL
 }
@@ -770,6 +1005,7 @@ struct Arena {
 };
 
 constexpr int64_t kPieceAlign = 256;
+constexpr int64_t kPad = 64;
 constexpr int64_t kMostBytes = int64_t(8) << 30;  // of a piece that `best` asks for
 constexpr int kMostSplits = 16;
 
@@ -784,8 +1020,9 @@ struct Layout {
     int shape;          // of the logits' product
     int dx_shape, dx_splits;
     // parts
-    int *index, *alive, *exponents, *row_exponent, *w_exponent;
+    int *index, *teacher_alive, *alive, *row_exponent, *w_exponent, *largest, *largest_w;
     float *weight, *factor, *entropy, *pick, *scale_x, *scale_w, *part_x;
+    int64_t ld_p;       // of P and w's transpose
     f32x2* part;
     char *x, *w, *p, *xt, *wt;
     fp16* q;
@@ -801,29 +1038,32 @@ Layout lay_out(const VocabArgs& a, bool grad, int64_t piece, Arena* arena) {
     l.piece = piece;
     l.pieces = std::max<int64_t>(1, (a.vocab + piece - 1) / piece);
     l.packed_ld = up(a.cols, 64);
-    l.rows_ld = up(a.rows, 64);
+    l.rows_ld = up(a.rows, 64) + kPad;
     l.planes = a.type == kF32 ? 2 : 1;
     l.pack_x = a.type == kF32 || !aligned_rows(a.x, a.x_stride, a.cols);
     l.pack_w = a.type == kF32 || !aligned_rows(a.w, a.w_stride, a.cols);
     const bool dx = grad && a.dx, dw = grad && a.dw;
     l.shape = choose_shape(std::min(piece, a.vocab), a.rows);
 
-    l.index = arena->take<int>(entries);
-    l.alive = arena->take<int>(a.rows);
+    l.ld_p = piece + kPad;
+    l.index = arena->take<int>(entries, a.top > 0);
     l.weight = arena->take<float>(entries, a.top > 0);
-    l.factor = arena->take<float>(a.rows, grad);
-    l.entropy = arena->take<float>(a.rows, !grad && a.top > 0);
-    l.pick = arena->take<float>(entries, !grad);
+    l.teacher_alive = arena->take<int>(a.rows, a.top > 0);
+    l.entropy = arena->take<float>(a.rows, a.top > 0);
     l.part = arena->take<f32x2>((a.vocab / (kTileRows[l.shape] / 2) + l.pieces) * a.rows, !grad);
-    l.exponents = arena->take<int>(1 + l.pieces);
+    l.alive = arena->take<int>(a.rows, grad);
+    l.factor = arena->take<float>(a.rows, grad);
+    l.pick = arena->take<float>(entries, grad || a.top > 0);
     l.row_exponent = arena->take<int>(a.rows, grad);
+    l.largest = arena->take<int>(kExponentBlocks, grad);
     l.scale_x = arena->take<float>(a.rows, a.type == kF32);
     l.scale_w = arena->take<float>(piece, a.type == kF32);
     l.w_exponent = arena->take<int>(piece, a.type == kF32);
+    l.largest_w = arena->take<int>(kExponentBlocks, a.type == kF32);
     l.x = arena->take<char>(l.planes * a.rows * l.packed_ld * 2, l.pack_x);
     l.w = arena->take<char>(l.planes * piece * l.packed_ld * 2, l.pack_w);
-    l.p = arena->take<char>(l.planes * a.rows * piece * 2, dx);
-    l.wt = arena->take<char>(l.planes * a.cols * piece * 2, dx);
+    l.p = arena->take<char>(l.planes * a.rows * l.ld_p * 2, dx);
+    l.wt = arena->take<char>(l.planes * a.cols * l.ld_p * 2, dx);
     l.q = arena->take<fp16>(2 * piece * l.rows_ld, dw);
     l.xt = arena->take<char>(l.planes * a.cols * l.rows_ld * 2, dw);
     if (dx) {
@@ -859,25 +1099,34 @@ int64_t choose_piece(const VocabArgs& a, bool grad, int64_t bytes) {
 
 // ---------------------------------------------------------- host: the passes
 
-hipError_t targets_of(const VocabArgs& a, const Layout& l, hipStream_t stream) {
-    const int n = int(1 + l.pieces);
-    if (a.top > 0)
-        hipLaunchKernelGGL(prepare_teacher, dim3(unsigned((a.rows + 3) / 4)), dim3(256),
-                           unsigned(a.top) * 32, stream, a.rows, a.vocab, a.top, a.target, a.logit,
-                           a.temperature, a.dloss, l.index, l.weight, l.alive, l.factor, l.entropy,
-                           l.exponents, n);
-    else
-        hipLaunchKernelGGL(prepare_targets, dim3(unsigned((a.rows + 255) / 256)), dim3(256), 0,
-                           stream, a.rows, a.vocab, a.target, a.dloss, l.index, l.alive, l.factor,
-                           l.exponents, n);
+Targets targets_of(const VocabArgs& a, const Layout& l) {
+    return {std::max(1, a.top), int(a.vocab), a.top ? nullptr : a.target, l.index, l.weight};
+}
+
+// A teacher's distribution and its entries' logits.
+template <typename S>
+hipError_t teacher_of(const VocabArgs& a, const Layout& l, hipStream_t stream) {
+    if (a.top == 0) return hipSuccess;
+    hipLaunchKernelGGL(prepare_teacher, dim3(unsigned((a.rows + 3) / 4)), dim3(256),
+                       unsigned(a.top) * 32, stream, a.rows, a.vocab, a.top, a.target, a.logit,
+                       a.temperature, l.index, l.weight, l.teacher_alive, l.entropy);
+    const int64_t waves = a.rows * ((a.top + kEntries - 1) / kEntries);
+    hipLaunchKernelGGL(target_logits<S>, dim3(unsigned((waves + 3) / 4)), dim3(256), 0, stream,
+                       static_cast<const S*>(a.x), a.x_stride, static_cast<const S*>(a.w), a.w_stride,
+                       a.rows, int(a.cols), targets_of(a, l), 1.0f / a.temperature, l.pick);
     return hipGetLastError();
+}
+
+// Blocks of four waves that take `rows` rows in turn.
+int row_blocks(int64_t rows) {
+    return int(std::min<int64_t>((rows + 3) / 4, kExponentBlocks));
 }
 
 template <typename S>
 hipError_t pack(const S* src, int64_t stride, int64_t rows, const VocabArgs& a, const Layout& l,
                 char* dst, int64_t plane_rows, float* scale, int* row_exponent, int* largest,
                 hipStream_t stream) {
-    hipLaunchKernelGGL(pack_rows<S>, dim3(unsigned((rows + 3) / 4)), dim3(256), 0, stream, src,
+    hipLaunchKernelGGL(pack_rows<S>, dim3(unsigned(row_blocks(rows))), dim3(256), 0, stream, src,
                        stride, rows, int(a.cols), static_cast<void*>(dst), l.packed_ld,
                        plane_rows * l.packed_ld, scale, row_exponent, largest);
     return hipGetLastError();
@@ -899,92 +1148,106 @@ PieceAt piece_at(const VocabArgs& a, const Layout& l, int64_t i) {
     return {i * l.piece, std::min(l.piece, a.vocab - i * l.piece)};
 }
 
-// The product that gives the logits of a piece, w's rows packed first where
-// they have to be.
+// The operands of a piece's logits, w's rows packed first where they have to
+// be.
 template <typename S>
-hipError_t logits_of(const VocabArgs& a, const Layout& l, int64_t i, Product* p, Logits* z,
-                     hipStream_t stream) {
+hipError_t logits_of(const VocabArgs& a, const Layout& l, int64_t i, Operand* x, Operand* w,
+                     Product* p, Logits* z, hipStream_t stream) {
     const PieceAt at = piece_at(a, l, i);
-    const S* const w = static_cast<const S*>(a.w) + at.first * a.w_stride;
+    const S* const from = static_cast<const S*>(a.w) + at.first * a.w_stride;
     if (l.pack_w) {
-        hipError_t e = pack(w, a.w_stride, at.rows, a, l, l.w, l.piece, l.scale_w, l.w_exponent,
-                            l.exponents + 1 + i, stream);
+        hipError_t e = pack(from, a.w_stride, at.rows, a, l, l.w, l.piece, l.scale_w, l.w_exponent,
+                            l.largest_w, stream);
         if (e != hipSuccess) return e;
-        p->r = {l.w, l.packed_ld, l.piece * l.packed_ld, int(at.rows)};
+        *w = {l.w, l.packed_ld, l.piece * l.packed_ld, int(at.rows)};
     } else {
-        p->r = {w, a.w_stride, 0, int(at.rows)};
+        *w = {from, a.w_stride, 0, int(at.rows)};
     }
     if (l.pack_x)
-        p->c = {l.x, l.packed_ld, a.rows * l.packed_ld, int(a.rows)};
+        *x = {l.x, l.packed_ld, a.rows * l.packed_ld, int(a.rows)};
     else
-        p->c = {a.x, a.x_stride, 0, int(a.rows)};
+        *x = {a.x, a.x_stride, 0, int(a.rows)};
     p->k = int(up(a.cols, 8));
     p->segments = l.planes == 2 ? 3 : 1;
-    *z = {int(a.rows), int(at.rows), int(at.first), 1.0f / a.temperature, l.scale_x, l.scale_w,
-          {std::max(1, a.top), l.index, l.weight}};
+    *z = {int(a.rows), int(at.rows), 1.0f / a.temperature, l.scale_x, l.scale_w};
     return hipSuccess;
 }
 
 // S: element type of x and w; T: of the products of logits and dx.
 template <typename S, typename T>
 hipError_t loss_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
-    hipError_t e = targets_of(a, l, stream);
+    hipError_t e = teacher_of<S>(a, l, stream);
     if (e == hipSuccess) e = pack_x<S>(a, l, stream);
     int blocks = 0;
     for (int64_t i = 0; i < l.pieces && e == hipSuccess; ++i) {
         Product p;
         Logits z;
-        e = logits_of<S>(a, l, i, &p, &z, stream);
+        e = logits_of<S>(a, l, i, &p.c, &p.r, &p, &z, stream);
         if (e != hipSuccess) break;
-        e = run_forward<T>(l.shape, p, z, {l.part, blocks, l.pick}, stream);
+        const ForwardOut o{l.part, blocks};
+        if constexpr (std::is_same<S, float>::value)
+            e = run_forward<T, true>(l.shape, p, z, o, stream);
+        else
+            e = a.temperature == 1.0f ? run_forward<T, false>(l.shape, p, z, o, stream)
+                                      : run_forward<T, true>(l.shape, p, z, o, stream);
         const int block = kTileRows[l.shape] / 2;
         blocks += (z.vocab + block - 1) / block;
     }
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(finish_loss, dim3(unsigned((a.rows + 63) / 64)), dim3(1024), 0, stream,
-                       l.part, blocks, a.rows, Targets{std::max(1, a.top), l.index, l.weight},
-                       l.pick, l.alive, l.entropy, a.temperature, a.loss, a.lse);
+    hipLaunchKernelGGL(finish_loss<S>, dim3(unsigned((a.rows + kFinishRows - 1) / kFinishRows)),
+                       dim3(1024), 0, stream, l.part, blocks, a.rows, static_cast<const S*>(a.x),
+                       a.x_stride, static_cast<const S*>(a.w), a.w_stride, int(a.cols),
+                       targets_of(a, l), l.pick, l.teacher_alive, l.entropy, a.temperature, a.loss,
+                       a.lse);
     return hipGetLastError();
 }
 
 template <typename S, typename T>
 hipError_t grad_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
     constexpr int PLANES = std::is_same<S, float>::value ? 2 : 1;
-    const dim3 by_tile_x(unsigned(l.rows_ld / 64), unsigned((a.cols + 63) / 64));
-    hipError_t e = targets_of(a, l, stream);
+    const Targets targets = targets_of(a, l);
+    const Largest largest{l.largest, row_blocks(a.rows)};
+    hipError_t e = teacher_of<S>(a, l, stream);
     if (e == hipSuccess) e = pack_x<S>(a, l, stream);
     if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(prepare_rows<S>, dim3(unsigned(row_blocks(a.rows))), dim3(256), 0, stream,
+                       static_cast<const S*>(a.x), a.x_stride, static_cast<const S*>(a.w),
+                       a.w_stride, a.rows, int(a.cols), targets, l.teacher_alive, a.dloss,
+                       a.temperature, l.alive, l.factor, l.pick, l.row_exponent, l.largest);
     if (a.dw) {
-        const int each = int(std::max<int64_t>(4, (a.rows + 511) / 512));
-        hipLaunchKernelGGL(row_exponents<S>, dim3(unsigned((a.rows + each - 1) / each)), dim3(256),
-                           0, stream, static_cast<const S*>(a.x), a.x_stride, a.rows, int(a.cols),
-                           each, l.factor, l.alive, l.row_exponent, l.exponents);
-        hipLaunchKernelGGL((transpose<S, true>), by_tile_x, dim3(256), 0, stream,
+        const dim3 by_tile(unsigned(up(a.rows, 64) / 64), unsigned((a.cols + 63) / 64));
+        hipLaunchKernelGGL((transpose<S, true>), by_tile, dim3(256), 0, stream,
                            static_cast<const S*>(a.x), a.x_stride, a.rows, int(a.cols),
                            static_cast<void*>(l.xt), l.rows_ld, a.cols * l.rows_ld, PLANES,
                            l.row_exponent, l.alive);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
     }
+    if ((e = hipGetLastError()) != hipSuccess) return e;
     for (int64_t i = 0; i < l.pieces; ++i) {
         const PieceAt at = piece_at(a, l, i);
-        const int* const largest_w = PLANES == 2 ? l.exponents + 1 + i : nullptr;
+        const Largest largest_w{l.largest_w, row_blocks(at.rows)};
         Product p;
         Logits z;
-        if ((e = logits_of<S>(a, l, i, &p, &z, stream)) != hipSuccess) return e;
-        BackwardOut o{a.lse, l.alive, l.factor, l.row_exponent, l.exponents, largest_w,
-                      l.p, l.piece, a.rows * l.piece, l.q, l.rows_ld, l.piece * l.rows_ld};
-        if ((e = run_backward<T, PLANES>(l.shape, p, z, o, stream)) != hipSuccess) return e;
+        if ((e = logits_of<S>(a, l, i, &p.r, &p.c, &p, &z, stream)) != hipSuccess) return e;
+        const BackwardOut o{a.lse, l.alive, l.factor, l.row_exponent, largest, largest_w,
+                            l.p, l.ld_p, a.rows * l.ld_p, l.q, l.rows_ld, l.piece * l.rows_ld};
+        e = a.dx && a.dw ? run_backward<T, PLANES, true>(l.shape, p, z, o, stream)
+                         : run_backward<T, PLANES, false>(l.shape, p, z, o, stream);
+        if (e != hipSuccess) return e;
+        const int64_t entries = a.rows * targets.top;
+        hipLaunchKernelGGL((take_targets<T, PLANES>), dim3(unsigned((entries + 255) / 256)), dim3(256),
+                           0, stream, targets, a.rows, int(at.first), int(at.rows), l.pick,
+                           l.scale_w, o);
         if (a.dx) {
             const int64_t k = up(at.rows, 64);
             const S* const w = static_cast<const S*>(a.w) + at.first * a.w_stride;
-            const dim3 by_tile_w(unsigned(k / 64), unsigned((a.cols + 63) / 64));
-            hipLaunchKernelGGL((transpose<S, PLANES == 2>), by_tile_w, dim3(256), 0, stream, w,
-                               a.w_stride, at.rows, int(a.cols), static_cast<void*>(l.wt), l.piece,
-                               a.cols * l.piece, PLANES, l.w_exponent, nullptr);
+            const dim3 by_tile(unsigned(k / 64), unsigned((a.cols + 63) / 64));
+            hipLaunchKernelGGL((transpose<S, PLANES == 2>), by_tile, dim3(256), 0, stream, w,
+                               a.w_stride, at.rows, int(a.cols), static_cast<void*>(l.wt), l.ld_p,
+                               a.cols * l.ld_p, PLANES, l.w_exponent, nullptr);
             if ((e = hipGetLastError()) != hipSuccess) return e;
             Product d;
-            d.r = {l.wt, l.piece, a.cols * l.piece, int(a.cols)};
-            d.c = {l.p, l.piece, a.rows * l.piece, int(a.rows)};
+            d.r = {l.wt, l.ld_p, a.cols * l.ld_p, int(a.cols)};
+            d.c = {l.p, l.ld_p, a.rows * l.ld_p, int(a.rows)};
             d.k = int(k);
             d.segments = PLANES == 2 ? 3 : 1;
             d.splits = l.dx_splits;
@@ -996,9 +1259,9 @@ hipError_t grad_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
             Product d;
             d.r = {l.xt, l.rows_ld, a.cols * l.rows_ld, int(a.cols)};
             d.c = {l.q, l.rows_ld, l.piece * l.rows_ld, int(at.rows)};
-            d.k = int(l.rows_ld);
+            d.k = int(up(a.rows, 64));
             d.segments = PLANES == 2 ? 3 : 2;
-            DwOut w{l.exponents, a.dw + at.first * a.dw_stride, a.dw_stride, a.accumulate,
+            DwOut w{largest, a.dw + at.first * a.dw_stride, a.dw_stride, a.accumulate,
                     int(at.rows), int(a.cols)};
             e = run_weights(choose_shape(a.cols, at.rows), d, w, stream);
             if (e != hipSuccess) return e;
