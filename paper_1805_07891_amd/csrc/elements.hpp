@@ -55,11 +55,28 @@ __device__ __forceinline__ void store_piece(T* p, const float* v, int n) {
     }
 }
 
-// Sum over the 64 lanes of a wave, in every lane.
+// Sum over the 64 lanes of a wave, in every lane (the same bits in each):
+// within rows of 16 lanes by DPP, then across them by exchanges, none of which waits for
+// LDS as a shuffle does.
+template <int CONTROL>
+__device__ __forceinline__ float add_dpp(float v) {
+    const int moved = __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CONTROL, 0xf, 0xf, true);
+    return v + __builtin_bit_cast(float, moved);
+}
+
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-    return v;
+    v = add_dpp<0xb1>(v);   // lane ^ 1
+    v = add_dpp<0x4e>(v);   // lane ^ 2
+    v = add_dpp<0x141>(v);  // the other half of 8 lanes
+    v = add_dpp<0x140>(v);  // the other half of 16
+    const uint32_t rows = __builtin_bit_cast(uint32_t, v);
+    const auto near = __builtin_amdgcn_permlane16_swap(rows, rows, false, false);
+    const uint32_t near0 = near[0], near1 = near[1];
+    v = __builtin_bit_cast(float, near0) + __builtin_bit_cast(float, near1);
+    const uint32_t halves = __builtin_bit_cast(uint32_t, v);
+    const auto far = __builtin_amdgcn_permlane32_swap(halves, halves, false, false);
+    const uint32_t far0 = far[0], far1 = far[1];
+    return __builtin_bit_cast(float, far0) + __builtin_bit_cast(float, far1);
 }
 
 }  // namespace

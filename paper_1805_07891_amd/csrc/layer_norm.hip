@@ -7,9 +7,10 @@
 // Bound by memory: forward reads x and writes y, backward reads dy and x and
 // writes dx, each once.  A row is read once and kept in registers between
 // its statistics and its result (the variance is taken about the mean, in
-// fp32).  kLanes threads share a row: one wave where a row fits its
-// registers (no barrier), a group of four or more for longer ones.
-// The backward pass's blocks each walk a strip of the rows, every thread
+// fp32), by one wave where that has the registers (no barrier), else by two to
+// sixteen.  Every load is a whole 16-byte vector and none is behind a branch,
+// so that all of a row's are in flight at once, and in the backward pass those of the next
+// row too.  The backward pass's blocks each walk a strip of the rows, every thread
 // owning the same columns in each, so the two weight gradients are summed in
 // registers; a strip's sums go to memory once and a second kernel adds the
 // strips in order, so the result does not change from run to run.
@@ -24,18 +25,20 @@
 namespace phub {
 namespace {
 
-constexpr int kStripBlocks = 256;  // one per compute unit
+// Strips of the backward pass: one block of eight waves per compute unit.  More
+// strips leave more partial sums (512: 8 us more for 8192 columns) and
+// are no faster otherwise.
+constexpr int kStripBlocks = 256;
 
 // Sum of v over the LANES threads that share a row.  Rows of one wave need
-// no barrier; others meet in LDS, two barriers apart so that the words can
-// be used again.
+// no barrier; others meet in LDS, where the words of one sum are not used again
+// before another sum's barrier.
 template <int LANES>
 __device__ __forceinline__ float row_sum(float v, float* words) {
     v = wave_sum(v);
     if constexpr (LANES > 64) {
         constexpr int W = LANES / 64;
         const int wave = int(threadIdx.x) / 64, first = wave / W * W;
-        __syncthreads();
         if ((threadIdx.x & 63) == 0) words[wave] = v;
         __syncthreads();
         v = 0.0f;
@@ -52,7 +55,6 @@ __device__ __forceinline__ f32x2 row_sum2(f32x2 v, f32x2* words) {
     if constexpr (LANES > 64) {
         constexpr int W = LANES / 64;
         const int wave = int(threadIdx.x) / 64, first = wave / W * W;
-        __syncthreads();
         if ((threadIdx.x & 63) == 0) words[wave] = v;
         __syncthreads();
         v = f32x2{0.0f, 0.0f};
@@ -82,38 +84,72 @@ __device__ __forceinline__ void load_floats(const float* p, int n, float fill, f
     }
 }
 
-template <typename T, int LANES, int PIECES>
+// A thread's piece of a row of at least kPerLoad columns, so that every load is
+// a whole vector and none is behind a branch (a wait would be at its end):
+// the row's last piece begins where it ends with the row and repeats
+// `skip` columns of the piece before; of a piece behind the row none counts.
+struct Span {
+    int c, skip;
+};
+
+template <typename T>
+__device__ __forceinline__ Span span(int nominal, int cols) {
+    constexpr int E = kPerLoad<T>;
+    const int c = min(nominal, cols - E);
+    return {c, nominal < cols ? nominal - c : E};
+}
+
+template <typename T>
+__device__ __forceinline__ Piece<T> whole_piece(const T* p) {
+    Piece<T> r;
+    __builtin_memcpy(&r, p, 16);
+    return r;
+}
+
+// EVEN: cols is a multiple of kPerLoad, no piece repeats columns.
+template <typename T, int LANES, int PIECES, bool EVEN>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_forward(NormArgs a) {
     constexpr int E = kPerLoad<T>, THREADS = LANES < 256 ? 256 : LANES;
-    __shared__ float words[THREADS / 64];
+    __shared__ float words[2][THREADS / 64];
     const int lane = int(threadIdx.x) % LANES;
     const int64_t row = int64_t(blockIdx.x) * (THREADS / LANES) + threadIdx.x / LANES;
-    if (row >= a.rows) return;  // LANES == 64 where a block has several rows: no barrier follows
+    // a row of one wave meets no barrier, the others' blocks stay whole
+    if (LANES <= 64 && row >= a.rows) return;
+    const bool live = row < a.rows;
     const int cols = int(a.cols);
-    const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+    const T* x = static_cast<const T*>(a.x) + (live ? row : 0) * a.x_stride;
     Piece<T> raw[PIECES];
+    Span at[PIECES];
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
-        const int c = (j * LANES + lane) * E;
-        raw[j] = load_piece<T>(x + c, cols - c);
+        at[j] = span<T>((j * LANES + lane) * E, cols);
+        raw[j] = whole_piece<T>(x + at[j].c);
     }
     float sum = 0.0f;
 #pragma unroll
-    for (int j = 0; j < PIECES; ++j)
+    for (int j = 0; j < PIECES; ++j) {
+        float part = 0.0f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum += float(raw[j].e[e]);
-    const float mean = row_sum<LANES>(sum, words) / float(cols);
+        for (int e = 0; e < E; ++e) {
+            const float v = float(raw[j].e[e]);
+            part += EVEN || e >= at[j].skip ? v : 0.0f;
+        }
+        sum += EVEN && at[j].skip ? 0.0f : part;
+    }
+    const float mean = row_sum<LANES>(sum, words[0]) / float(cols);
     float sq = 0.0f;
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
-        const int n = cols - (j * LANES + lane) * E;
+        float part = 0.0f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const float d = float(raw[j].e[e]) - mean;
-            if (e < n) sq = __builtin_fmaf(d, d, sq);
+            const float v = float(raw[j].e[e]) - mean, d = EVEN || e >= at[j].skip ? v : 0.0f;
+            part = __builtin_fmaf(d, d, part);
         }
+        sq += EVEN && at[j].skip ? 0.0f : part;
     }
-    const float rstd = 1.0f / __builtin_sqrtf(row_sum<LANES>(sq, words) / float(cols) + a.eps);
+    const float rstd = 1.0f / __builtin_sqrtf(row_sum<LANES>(sq, words[1]) / float(cols) + a.eps);
+    if (!live) return;
     if (lane == 0) {
         if (a.mean) a.mean[row] = mean;
         if (a.rstd) a.rstd[row] = rstd;
@@ -121,24 +157,24 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_forward(NormAr
     T* y = static_cast<T*>(a.y) + row * a.y_stride;
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
-        const int c = (j * LANES + lane) * E, n = cols - c;
-        if (n <= 0) break;
+        const int c = at[j].c;
+        if (at[j].skip == E) break;
         float w[E], b[E];
-        load_floats<T>(a.weight ? a.weight + c : nullptr, n, 1.0f, w);
-        load_floats<T>(a.bias ? a.bias + c : nullptr, n, 0.0f, b);
+        load_floats<T>(a.weight ? a.weight + c : nullptr, E, 1.0f, w);
+        load_floats<T>(a.bias ? a.bias + c : nullptr, E, 0.0f, b);
 #pragma unroll
         for (int e = 0; e < E; ++e)
             w[e] = __builtin_fmaf((float(raw[j].e[e]) - mean) * rstd, w[e], b[e]);
-        store_piece<T>(y + c, w, n);
+        store_piece<T>(y + c, w, E);  // repeated columns get the same values twice
     }
 }
 
-// Rows that do not fit the registers: read three times, the second and third
-// time mostly from the caches.
+// Rows that do not fit the registers, and those shorter than a piece: read
+// three times, the second and third time mostly from the caches.
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_forward_long(NormArgs a) {
     constexpr int E = kPerLoad<T>, LANES = 1024;
-    __shared__ float words[LANES / 64];
+    __shared__ float words[2][LANES / 64];
     const int lane = int(threadIdx.x);
     const int64_t row = blockIdx.x, cols = a.cols;
     const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
@@ -148,7 +184,7 @@ __global__ __launch_bounds__(1024) void norm_forward_long(NormArgs a) {
 #pragma unroll
         for (int e = 0; e < E; ++e) sum += float(p.e[e]);
     }
-    const float mean = row_sum<LANES>(sum, words) / float(cols);
+    const float mean = row_sum<LANES>(sum, words[0]) / float(cols);
     for (int64_t c = lane * E; c < cols; c += LANES * E) {
         const Piece<T> p = load_piece<T>(x + c, int(cols - c));
 #pragma unroll
@@ -157,7 +193,7 @@ __global__ __launch_bounds__(1024) void norm_forward_long(NormArgs a) {
             if (c + e < cols) sq = __builtin_fmaf(d, d, sq);
         }
     }
-    const float rstd = 1.0f / __builtin_sqrtf(row_sum<LANES>(sq, words) / float(cols) + a.eps);
+    const float rstd = 1.0f / __builtin_sqrtf(row_sum<LANES>(sq, words[1]) / float(cols) + a.eps);
     if (lane == 0) {
         if (a.mean) a.mean[row] = mean;
         if (a.rstd) a.rstd[row] = rstd;
@@ -178,73 +214,84 @@ __global__ __launch_bounds__(1024) void norm_forward_long(NormArgs a) {
 
 // A block's THREADS / LANES groups of threads take the rows in turn; block b
 // has rows b, b + gridDim.x, ... of groups of rows.
-template <typename T, int LANES, int PIECES>
+template <typename T, int LANES, int PIECES, bool EVEN>
 __global__ __launch_bounds__(512) void norm_backward(NormArgs a) {
     constexpr int E = kPerLoad<T>, THREADS = 512;
     constexpr int GROUPS = THREADS / LANES;
-    __shared__ f32x2 words[THREADS / 64];
+    __shared__ f32x2 words[2][THREADS / 64];
     const int lane = int(threadIdx.x) % LANES, group = int(threadIdx.x) / LANES;
     const int cols = int(a.cols);
     float w[PIECES][E], dw[PIECES][E], db[PIECES][E];
+    Span at[PIECES];
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
-        const int c = (j * LANES + lane) * E;
-        load_floats<T>(a.weight ? a.weight + c : nullptr, cols - c, 1.0f, w[j]);
+        at[j] = span<T>((j * LANES + lane) * E, cols);
+        load_floats<T>(a.weight ? a.weight + at[j].c : nullptr, E, 1.0f, w[j]);
 #pragma unroll
         for (int e = 0; e < E; ++e) dw[j][e] = db[j][e] = 0.0f;
     }
-    // every group makes the same number of turns (barriers inside)
+    // every group makes the same number of turns (barriers inside); the next
+    // turn's rows are on their way while this one's are summed and written
     const int64_t turns = (a.rows + GROUPS - 1) / GROUPS;
-    for (int64_t turn = blockIdx.x; turn < turns; turn += gridDim.x) {
+    Piece<T> nx[PIECES], nd[PIECES];
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    auto load = [&](int64_t turn) {
+        const int64_t row = std::min<int64_t>(turn * GROUPS + group, a.rows - 1);
+        const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+        const T* dy = static_cast<const T*>(a.dy) + row * a.dy_stride;
+        next_mean = a.mean[row];
+        next_rstd = a.rstd[row];
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) {
+            nx[j] = whole_piece<T>(x + at[j].c);
+            nd[j] = whole_piece<T>(dy + at[j].c);
+        }
+    };
+    constexpr bool AHEAD = PIECES * E <= 16;  // with more there are no registers for it
+    if (AHEAD) load(blockIdx.x);
+    int odd = 0;
+    for (int64_t turn = blockIdx.x; turn < turns; turn += gridDim.x, odd ^= 1) {
         const int64_t row = turn * GROUPS + group;
         const bool live = row < a.rows;
+        if (!AHEAD) load(turn);
         Piece<T> rx[PIECES], rd[PIECES];
-        float mean = 0.0f, rstd = 0.0f;
-        if (live) {
-            const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
-            const T* dy = static_cast<const T*>(a.dy) + row * a.dy_stride;
-            mean = a.mean[row];
-            rstd = a.rstd[row];
 #pragma unroll
-            for (int j = 0; j < PIECES; ++j) {
-                const int c = (j * LANES + lane) * E;
-                rx[j] = load_piece<T>(x + c, cols - c);
-                rd[j] = load_piece<T>(dy + c, cols - c);
-            }
-        } else {
+        for (int j = 0; j < PIECES; ++j) {
+            rx[j] = nx[j];
+            rd[j] = nd[j];
+        }
+        const float mean = next_mean, rstd = next_rstd;
+        if (AHEAD) load(turn + gridDim.x);
+        f32x2 s = {0.0f, 0.0f};  // sums of dy w and of dy w h
+        if (live) {
 #pragma unroll
             for (int j = 0; j < PIECES; ++j)
 #pragma unroll
-                for (int e = 0; e < E; ++e) rx[j].e[e] = rd[j].e[e] = T(0.0f);
+                for (int e = 0; e < E; ++e) {
+                    const bool counts = EVEN ? at[j].skip == 0 : e >= at[j].skip;
+                    const float d = counts ? float(rd[j].e[e]) : 0.0f;
+                    const float h = counts ? (float(rx[j].e[e]) - mean) * rstd : 0.0f;
+                    const float g = d * w[j][e];
+                    s.x += g;
+                    s.y = __builtin_fmaf(g, h, s.y);
+                    dw[j][e] = __builtin_fmaf(d, h, dw[j][e]);
+                    db[j][e] += d;
+                }
         }
-        f32x2 s = {0.0f, 0.0f};  // sums of dy w and of dy w h
-#pragma unroll
-        for (int j = 0; j < PIECES; ++j)
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                // columns past the end have dy = 0 and a finite h
-                const float d = float(rd[j].e[e]), h = (float(rx[j].e[e]) - mean) * rstd;
-                const float g = d * w[j][e];
-                s.x += g;
-                s.y = __builtin_fmaf(g, h, s.y);
-                dw[j][e] = __builtin_fmaf(d, h, dw[j][e]);
-                db[j][e] += d;
-            }
-        s = row_sum2<LANES>(s, words);
+        s = row_sum2<LANES>(s, words[odd]);
         if (live && a.y) {
             const float c1 = s.x / float(cols), c2 = s.y / float(cols);
             T* dx = static_cast<T*>(a.y) + row * a.y_stride;
 #pragma unroll
             for (int j = 0; j < PIECES; ++j) {
-                const int c = (j * LANES + lane) * E, n = cols - c;
-                if (n <= 0) break;
+                if (at[j].skip == E) break;
                 float v[E];
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     const float d = float(rd[j].e[e]), h = (float(rx[j].e[e]) - mean) * rstd;
                     v[e] = rstd * (__builtin_fmaf(d, w[j][e], -c1) - h * c2);
                 }
-                store_piece<T>(dx + c, v, n);
+                store_piece<T>(dx + at[j].c, v, E);  // repeated columns get the same values twice
             }
         }
     }
@@ -272,13 +319,19 @@ __global__ __launch_bounds__(512) void norm_backward(NormArgs a) {
                         db[j][e] += o.y;
                     }
         }
-        const int c = (j * LANES + lane) * E, n = cols - c;
-        if (group == 0 && n > 0) {
+        if (group == 0 && at[j].skip == 0) {
 #pragma unroll
             for (int e = 0; e < E; e += 4) {
-                store_piece<float>(pw + c + e, dw[j] + e, n - e);
-                store_piece<float>(pb + c + e, db[j] + e, n - e);
+                store_piece<float>(pw + at[j].c + e, dw[j] + e, 4);
+                store_piece<float>(pb + at[j].c + e, db[j] + e, 4);
             }
+        } else if (!EVEN && group == 0) {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (e >= at[j].skip) {
+                    pw[at[j].c + e] = dw[j][e];
+                    pb[at[j].c + e] = db[j][e];
+                }
         }
     }
 }
@@ -351,23 +404,27 @@ __global__ __launch_bounds__(256) void norm_strip_sums(NormArgs a) {
     }
 }
 
-// Adds the strips' sums, 64 columns a block, a quarter of the strips a wave;
+// Adds the strips' sums, 64 columns a block, the strips dealt to its sixteen waves;
 // blockIdx.y: 0 the weight's, 1 the bias's.
-__global__ __launch_bounds__(256) void norm_join(const float* partial, int64_t strips, int64_t cols,
-                                                 float* dweight, float* dbias, bool accumulate) {
-    __shared__ float part[4][64];
+__global__ __launch_bounds__(1024) void norm_join(const float* partial, int strips, int64_t cols,
+                                                  float* dweight, float* dbias, bool accumulate) {
+    __shared__ float part[16][64];
     float* const out = blockIdx.y ? dbias : dweight;
     if (!out) return;
     const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) / 64;
     const int64_t c = int64_t(blockIdx.x) * 64 + lane;
     const float* p = partial + int64_t(blockIdx.y) * strips * cols;
     float s = 0.0f;
-    if (c < cols)
-        for (int64_t i = wave; i < strips; i += 4) s += p[i * cols + c];
+    if (c < cols) {
+#pragma unroll 16
+        for (int i = wave; i < strips; i += 16) s += p[int64_t(i) * cols + c];
+    }
     part[wave][lane] = s;
     __syncthreads();
     if (wave == 0 && c < cols) {
-        s = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
+        s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += part[i][lane];
         out[c] = accumulate ? out[c] + s : s;
     }
 }
@@ -380,56 +437,72 @@ __global__ __launch_bounds__(256) void norm_clear(int64_t cols, float* dweight, 
     if (dbias) dbias[c] = 0.0f;
 }
 
-// Threads of a row, and 16-byte pieces a thread keeps of it: one wave up to
-// 4 pieces a lane, then four waves up to 4; then sixteen waves with 2 pieces
-// forward and, as the backward pass needs five times the registers, eight
-// waves with 4.  Longer rows are not kept.
-template <typename T>
-bool is_long(int64_t cols) {
-    return cols > 2 * 1024 * kPerLoad<T>;
+template <typename T, int LANES, int PIECES>
+void launch_forward(const NormArgs& a, hipStream_t stream) {
+    constexpr int THREADS = LANES < 256 ? 256 : LANES, ROWS = THREADS / LANES;
+    const dim3 grid(unsigned((a.rows + ROWS - 1) / ROWS));
+    if (a.cols % kPerLoad<T> == 0)
+        hipLaunchKernelGGL((norm_forward<T, LANES, PIECES, true>), grid, dim3(THREADS), 0, stream, a);
+    else
+        hipLaunchKernelGGL((norm_forward<T, LANES, PIECES, false>), grid, dim3(THREADS), 0, stream, a);
 }
 
+template <typename T, int LANES, int ELEMENTS>
+void launch_backward(const NormArgs& a, int64_t strips, hipStream_t stream) {
+    if (a.cols % kPerLoad<T> == 0)
+        hipLaunchKernelGGL((norm_backward<T, LANES, ELEMENTS / kPerLoad<T>, true>),
+                           dim3(unsigned(strips)), dim3(512), 0, stream, a);
+    else
+        hipLaunchKernelGGL((norm_backward<T, LANES, ELEMENTS / kPerLoad<T>, false>),
+                           dim3(unsigned(strips)), dim3(512), 0, stream, a);
+}
+
+// Forward a thread keeps two pieces of a row, and as many threads share the
+// row as that takes.  (16384 x 4096 bf16, 256 threads with two pieces: 43.5 us, 6.2 TB/s; 512 with
+// one: 48.0; fp32, 512 with two: 94.4, 256 with four: 103.8; 8192 x 8192 bf16, 512 with
+// two: 42.8, 256 with four: 44.7, 1024 with one: 52.4.)
 template <typename T>
 hipError_t forward(const NormArgs& a, hipStream_t stream) {
     const int64_t pieces = (a.cols + kPerLoad<T> - 1) / kPerLoad<T>;
-    const dim3 by_row(unsigned(a.rows)), by_four(unsigned((a.rows + 3) / 4));
-    if (pieces <= 64) {
-        hipLaunchKernelGGL((norm_forward<T, 64, 1>), by_four, dim3(256), 0, stream, a);
-    } else if (pieces <= 128) {
-        hipLaunchKernelGGL((norm_forward<T, 64, 2>), by_four, dim3(256), 0, stream, a);
-    } else if (pieces <= 256) {
-        hipLaunchKernelGGL((norm_forward<T, 64, 4>), by_four, dim3(256), 0, stream, a);
-    } else if (pieces <= 512) {
-        hipLaunchKernelGGL((norm_forward<T, 256, 2>), by_row, dim3(256), 0, stream, a);
-    } else if (pieces <= 1024) {
-        hipLaunchKernelGGL((norm_forward<T, 256, 4>), by_row, dim3(256), 0, stream, a);
-    } else if (!is_long<T>(a.cols)) {
-        hipLaunchKernelGGL((norm_forward<T, 1024, 2>), by_row, dim3(1024), 0, stream, a);
-    } else {
-        hipLaunchKernelGGL(norm_forward_long<T>, by_row, dim3(1024), 0, stream, a);
-    }
+    if (a.cols < kPerLoad<T> || pieces > 2048)
+        hipLaunchKernelGGL(norm_forward_long<T>, dim3(unsigned(a.rows)), dim3(1024), 0, stream, a);
+    else if (pieces <= 64)
+        launch_forward<T, 64, 1>(a, stream);
+    else if (pieces <= 128)
+        launch_forward<T, 64, 2>(a, stream);
+    else if (pieces <= 256)
+        launch_forward<T, 128, 2>(a, stream);
+    else if (pieces <= 512)
+        launch_forward<T, 256, 2>(a, stream);
+    else if (pieces <= 1024)
+        launch_forward<T, 512, 2>(a, stream);
+    else
+        launch_forward<T, 1024, 2>(a, stream);
     return hipGetLastError();
 }
 
+// The backward pass keeps 16 elements a thread with the weights, two sums and
+// the next row's elements beside them (118 registers for 16-bit types); 8192 x 8192 bf16 80 us, 5.0
+// TB/s; 16384 x 4096 fp32 151 us, 5.3 TB/s.
 template <typename T>
 hipError_t backward(NormArgs a, hipStream_t stream) {
-    const int64_t pieces = (a.cols + kPerLoad<T> - 1) / kPerLoad<T>;
     const int64_t strips = norm_strips(a.rows, a.cols);
-    const dim3 grid{unsigned(strips)};
     if (!a.dweight && !a.dbias) a.partial = nullptr;
-    if (pieces <= 64) {
-        hipLaunchKernelGGL((norm_backward<T, 64, 1>), grid, dim3(512), 0, stream, a);
-    } else if (pieces <= 128) {
-        hipLaunchKernelGGL((norm_backward<T, 64, 2>), grid, dim3(512), 0, stream, a);
-    } else if (pieces <= 256) {
-        hipLaunchKernelGGL((norm_backward<T, 64, 4>), grid, dim3(512), 0, stream, a);
-    } else if (pieces <= 512) {
-        hipLaunchKernelGGL((norm_backward<T, 256, 2>), grid, dim3(512), 0, stream, a);
-    } else if (pieces <= 1024) {
-        hipLaunchKernelGGL((norm_backward<T, 256, 4>), grid, dim3(512), 0, stream, a);
-    } else if (!is_long<T>(a.cols)) {
-        hipLaunchKernelGGL((norm_backward<T, 512, 4>), grid, dim3(512), 0, stream, a);
+    const bool kept = a.cols >= kPerLoad<T>;
+    if (kept && a.cols <= 512) {
+        launch_backward<T, 64, 8>(a, strips, stream);
+    } else if (kept && a.cols <= 1024) {
+        launch_backward<T, 64, 16>(a, strips, stream);
+    } else if (kept && a.cols <= 2048) {
+        launch_backward<T, 128, 16>(a, strips, stream);
+    } else if (kept && a.cols <= 4096) {
+        launch_backward<T, 256, 16>(a, strips, stream);
+    } else if (kept && a.cols <= 8192) {
+        launch_backward<T, 512, 16>(a, strips, stream);
+    } else if (kept && a.cols <= 16384) {
+        launch_backward<T, 512, 32>(a, strips, stream);
     } else {
+        const int64_t pieces = (a.cols + kPerLoad<T> - 1) / kPerLoad<T>;
         if (a.y)
             hipLaunchKernelGGL(norm_backward_long<T>, dim3(unsigned(a.rows)), dim3(1024), 0, stream, a);
         if (a.partial)
@@ -439,8 +512,8 @@ hipError_t backward(NormArgs a, hipStream_t stream) {
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.partial) return e;
-    hipLaunchKernelGGL(norm_join, dim3(unsigned((a.cols + 63) / 64), 2), dim3(256), 0, stream,
-                       a.partial, strips, a.cols, a.dweight, a.dbias, a.accumulate);
+    hipLaunchKernelGGL(norm_join, dim3(unsigned((a.cols + 63) / 64), 2), dim3(1024), 0, stream,
+                       a.partial, int(strips), a.cols, a.dweight, a.dbias, a.accumulate);
     return hipGetLastError();
 }
 

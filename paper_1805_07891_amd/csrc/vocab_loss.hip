@@ -847,33 +847,37 @@ __global__ __launch_bounds__(kProductThreads) void grad_rows(Product p, DxOut ou
     }
 }
 
-// Adds the parts of dx and gives it its rows' factors.
+// Adds the parts of a product: times the rows' factors (null: 1), to what is
+// there if asked.
 template <typename O>
-__global__ __launch_bounds__(256) void join_rows(const float* part, int splits, int64_t rows,
-                                                 int64_t cols, const float* factor, O* dx,
-                                                 int64_t stride) {
+__global__ __launch_bounds__(256) void join_parts(const float* part, int splits, int64_t rows,
+                                                  int64_t cols, const float* factor, bool add, O* out,
+                                                  int64_t stride) {
     const int64_t c = (int64_t(blockIdx.y) * 256 + threadIdx.x) * 4, row = blockIdx.x;
     if (c >= cols) return;
     const int n = int(std::min<int64_t>(4, cols - c));
     float v[4] = {};
+#pragma unroll 4
     for (int s = 0; s < splits; ++s) {
         const Piece<float> r = load_piece<float>(part + (s * rows + row) * cols + c, n);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] += r.e[e];
     }
-    const float f = factor[row];
+    const float f = factor ? factor[row] : 1.0f;
+    O* const to = out + row * stride + c;
     f32x4 o;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = v[e] * f;
-    store4(dx + row * stride + c, o, n, true);
+    for (int e = 0; e < 4; ++e) o[e] = v[e] * f + (add && e < n ? float(to[e]) : 0.0f);
+    store4(to, o, n, true);
 }
 
 struct DwOut {
     Largest largest;
-    float* dw;
+    float* dw;         // null: to parts
     int64_t stride;
-    bool add;
-    int vocab, cols;  // valid rows of this piece, columns
+    bool add;          // to what dw holds
+    float* part;       // [splits][vocab][cols]
+    int vocab, cols;   // valid rows of this piece, columns
 };
 
 template <int WR, int WC, int STAGES>
@@ -900,7 +904,8 @@ __global__ __launch_bounds__(kProductThreads) void grad_weights(Product p, DwOut
                 f32x4 y;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) y[e] = __builtin_amdgcn_ldexpf(acc[i][j][g * 4 + e], e2);
-                float* const to = out.dw + int64_t(v) * out.stride + c;
+                float* const to = out.dw ? out.dw + int64_t(v) * out.stride + c
+                                         : out.part + (int64_t(at.split) * out.vocab + v) * out.cols + c;
                 if (out.add)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) y[e] += c + e < out.cols ? to[e] : 0.0f;
@@ -917,30 +922,49 @@ __global__ __launch_bounds__(256) void clear_weights(float* dw, int64_t stride, 
 
 // ------------------------------------------------------------- host: tiles
 
-// Tile shapes: 256 x 256 where the product has enough such tiles to fill the
-// chip, else 128 x 128, else 64 x 64.
+// Tile shapes, and how many parts the k loop is cut into where few tiles have a
+// long one.  A block has a compute unit to itself (its stages take 128 KiB of
+// LDS), so a product takes as many rounds as its blocks fill the chip, each as long as
+// one block's loop.  Measured us for 64 of k and for the rest of a block:
+//   256 x 256   1.4 (all units at work; 1.3 alone)   6
+//   128 x 128   0.55                                 3
+//    64 x  64   0.30                                 2
+// e.g. 64 rows, 4096 columns, 32768 entries: 103, 66 and 70 us for a whole loss (the three
+// shapes); 512, 4096, 8192: 97, 55, 82; 2048, 4096, 8192: 130, 151, 253.
 enum Shape { kBig = 0, kMid = 1, kSmall = 2 };
 constexpr int kTileRows[] = {256, 128, 64};
-#ifndef ST0
-#define ST0 4
-#define ST1 4
-#define ST2 4
-#endif
-constexpr int kStages[] = {ST0, ST1, ST2};
+constexpr float kStepCost[] = {1.4f, 0.55f, 0.30f};
+constexpr float kBlockCost[] = {6.0f, 3.0f, 2.0f};
+constexpr int kStages[] = {4, 4, 4};
 constexpr int kUnits = 256;  // compute units
+constexpr int kMostSplits = 32;
+constexpr float kJoinCost = 4.0f, kJoinBytes = 4e6f;  // us of a launch; bytes a us
 
-int64_t tiles_of(int shape, int64_t r, int64_t c) {
-    const int n = kTileRows[shape];
-    return ((r + n - 1) / n) * ((c + n - 1) / n);
-}
+struct Plan {
+    int shape = kSmall, splits = 1;
+};
 
-int choose_shape(int64_t r, int64_t c) {
-#ifdef FORCE_SHAPE
-    return FORCE_SHAPE;
-#endif
-    for (int s = kBig; s < kSmall; ++s)
-        if (tiles_of(s, r, c) >= kUnits * 3 / 4) return s;
-    return kSmall;
+// The cheapest shape and number of parts for an r x c product over `steps` x 64 of k.
+Plan choose_plan(int64_t r, int64_t c, int64_t steps, bool may_split) {
+    Plan best;
+    float least = __builtin_huge_valf();
+    for (int shape = kBig; shape <= kSmall; ++shape) {
+        const int n = kTileRows[shape];
+        const int64_t tiles = ((r + n - 1) / n) * ((c + n - 1) / n);
+        for (int splits = 1; splits <= (may_split ? kMostSplits : 1); splits *= 2) {
+            if (splits > 1 && (tiles * splits > 2 * kUnits || steps < 4 * splits)) break;
+            const int64_t rounds = (tiles * splits + kUnits - 1) / kUnits;
+            float cost = float(rounds) * (float(steps) / float(splits) * kStepCost[shape] + kBlockCost[shape]);
+            // parts are written and read in fp32, and joined by a kernel
+            if (splits > 1) cost += kJoinCost + float(splits) * float(r) * float(c) * 8.0f / kJoinBytes;
+            if (cost < least) {
+                least = cost;
+                best.shape = shape;
+                best.splits = splits;
+            }
+        }
+    }
+    return best;
 }
 
 template <int WR, int WC, typename K, typename... A>
@@ -1007,7 +1031,6 @@ struct Arena {
 constexpr int64_t kPieceAlign = 256;
 constexpr int64_t kPad = 64;
 constexpr int64_t kMostBytes = int64_t(8) << 30;  // of a piece that `best` asks for
-constexpr int kMostSplits = 16;
 
 struct Layout {
     // sizes
@@ -1018,10 +1041,10 @@ struct Layout {
     bool pack_x, pack_w;
     int planes;         // 2: fp32
     int shape;          // of the logits' product
-    int dx_shape, dx_splits;
+    Plan dx_plan, dw_plan;
     // parts
     int *index, *teacher_alive, *alive, *row_exponent, *w_exponent, *largest, *largest_w;
-    float *weight, *factor, *entropy, *pick, *scale_x, *scale_w, *part_x;
+    float *weight, *factor, *entropy, *pick, *scale_x, *scale_w, *part_x, *part_w;
     int64_t ld_p;       // of P and w's transpose
     f32x2* part;
     char *x, *w, *p, *xt, *wt;
@@ -1043,7 +1066,9 @@ Layout lay_out(const VocabArgs& a, bool grad, int64_t piece, Arena* arena) {
     l.pack_x = a.type == kF32 || !aligned_rows(a.x, a.x_stride, a.cols);
     l.pack_w = a.type == kF32 || !aligned_rows(a.w, a.w_stride, a.cols);
     const bool dx = grad && a.dx, dw = grad && a.dw;
-    l.shape = choose_shape(std::min(piece, a.vocab), a.rows);
+    const int64_t most = std::min(piece, a.vocab);  // rows of w in a piece
+    const int64_t steps = (a.cols + 63) / 64;
+    l.shape = choose_plan(most, a.rows, steps * (l.planes == 2 ? 3 : 1), false).shape;
 
     l.ld_p = piece + kPad;
     l.index = arena->take<int>(entries, a.top > 0);
@@ -1067,12 +1092,14 @@ Layout lay_out(const VocabArgs& a, bool grad, int64_t piece, Arena* arena) {
     l.q = arena->take<fp16>(2 * piece * l.rows_ld, dw);
     l.xt = arena->take<char>(l.planes * a.cols * l.rows_ld * 2, dw);
     if (dx) {
-        l.dx_shape = choose_shape(a.cols, a.rows);
-        const int64_t tiles = tiles_of(l.dx_shape, a.cols, a.rows);
-        const int64_t steps = l.planes * up(std::min(piece, a.vocab), 64) / 64;
-        l.dx_splits = int(std::max<int64_t>(1, std::min<int64_t>({kMostSplits, kUnits / tiles, steps / 8})));
-        l.part_x = arena->take<float>(int64_t(l.dx_splits) * a.rows * a.cols,
-                                      l.dx_splits > 1 || l.pieces > 1);
+        l.dx_plan = choose_plan(a.cols, a.rows, (most + 63) / 64 * (l.planes == 2 ? 3 : 1), true);
+        l.part_x = arena->take<float>(int64_t(l.dx_plan.splits) * a.rows * a.cols,
+                                      l.dx_plan.splits > 1 || l.pieces > 1);
+    }
+    if (dw) {
+        l.dw_plan = choose_plan(a.cols, most, (a.rows + 63) / 64 * (l.planes == 2 ? 3 : 2), true);
+        l.part_w = arena->take<float>(int64_t(l.dw_plan.splits) * most * a.cols,
+                                      l.dw_plan.splits > 1);
     }
     return l;
 }
@@ -1138,6 +1165,14 @@ hipError_t pack_x(const VocabArgs& a, const Layout& l, hipStream_t stream) {
     if (!l.pack_x) return hipSuccess;
     return pack(static_cast<const S*>(a.x), a.x_stride, a.rows, a, l, l.x, a.rows, l.scale_x,
                 static_cast<int*>(nullptr), static_cast<int*>(nullptr), stream);
+}
+
+template <typename O>
+hipError_t join(const float* part, int splits, int64_t rows, const VocabArgs& a, const float* factor,
+                bool add, O* out, int64_t stride, hipStream_t stream) {
+    hipLaunchKernelGGL(join_parts<O>, dim3(unsigned(rows), unsigned((a.cols + 1023) / 1024)), dim3(256),
+                       0, stream, part, splits, rows, a.cols, factor, add, out, stride);
+    return hipGetLastError();
 }
 
 struct PieceAt {
@@ -1250,10 +1285,10 @@ hipError_t grad_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
             d.c = {l.p, l.ld_p, a.rows * l.ld_p, int(a.rows)};
             d.k = int(k);
             d.segments = PLANES == 2 ? 3 : 1;
-            d.splits = l.dx_splits;
+            d.splits = l.dx_plan.splits;
             DxOut x{l.alive, l.factor, largest_w, l.part_x ? nullptr : a.dx, a.dx_stride, l.part_x,
                     i > 0, int(a.rows), int(a.cols)};
-            if ((e = run_rows<T, S>(l.dx_shape, d, x, stream)) != hipSuccess) return e;
+            if ((e = run_rows<T, S>(l.dx_plan.shape, d, x, stream)) != hipSuccess) return e;
         }
         if (a.dw) {
             Product d;
@@ -1261,18 +1296,20 @@ hipError_t grad_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
             d.c = {l.q, l.rows_ld, l.piece * l.rows_ld, int(at.rows)};
             d.k = int(up(a.rows, 64));
             d.segments = PLANES == 2 ? 3 : 2;
-            DwOut w{largest, a.dw + at.first * a.dw_stride, a.dw_stride, a.accumulate,
-                    int(at.rows), int(a.cols)};
-            e = run_weights(choose_shape(a.cols, at.rows), d, w, stream);
-            if (e != hipSuccess) return e;
+            d.splits = l.dw_plan.splits;
+            float* const dw = a.dw + at.first * a.dw_stride;
+            const DwOut w{largest, l.part_w ? nullptr : dw, a.dw_stride, a.accumulate && !l.part_w,
+                          l.part_w, int(at.rows), int(a.cols)};
+            if ((e = run_weights(l.dw_plan.shape, d, w, stream)) != hipSuccess) return e;
+            if (l.part_w) {
+                e = join(l.part_w, d.splits, at.rows, a, nullptr, a.accumulate, dw, a.dw_stride, stream);
+                if (e != hipSuccess) return e;
+            }
         }
     }
-    if (a.dx && l.part_x) {
-        hipLaunchKernelGGL(join_rows<S>, dim3(unsigned(a.rows), unsigned((a.cols + 1023) / 1024)),
-                           dim3(256), 0, stream, l.part_x, l.dx_splits, a.rows, a.cols, l.factor,
-                           static_cast<S*>(a.dx), a.dx_stride);
-        e = hipGetLastError();
-    }
+    if (a.dx && l.part_x)
+        e = join(l.part_x, l.dx_plan.splits, a.rows, a, l.factor, false, static_cast<S*>(a.dx),
+                 a.dx_stride, stream);
     return e;
 }
 

@@ -292,15 +292,17 @@ class Library:
 
     # -- the worker's operators (pointers as ints; see phub.h) ---------------
     def phub_layer_norm(self, *args, check: bool = True) -> int:
-        return self._check(self.lib.phub_layer_norm(*args), check)
+        rc = self.lib.phub_layer_norm(*args)
+        return rc if not rc else self._check(rc, check)
 
     def phub_layer_norm_grad_bytes(self, rows: int, cols: int) -> int:
         out = ctypes.c_int64()
-        self._check(self.lib.phub_layer_norm_grad_bytes(int(rows), int(cols), ctypes.byref(out)), True)
+        self._check(self.lib.phub_layer_norm_grad_bytes(rows, cols, ctypes.byref(out)), True)
         return out.value
 
     def phub_layer_norm_grad(self, *args, check: bool = True) -> int:
-        return self._check(self.lib.phub_layer_norm_grad(*args), check)
+        rc = self.lib.phub_layer_norm_grad(*args)
+        return rc if not rc else self._check(rc, check)
 
     def phub_vocab_bytes(self, *args):
         """(least, best) bytes of workspace."""
