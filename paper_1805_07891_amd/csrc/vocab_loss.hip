@@ -11,15 +11,16 @@
 //   G = g T (softmax(z) - q),   dx = G w,   dw = G^T x.
 //
 // Forward: each tile of the product leaves, for every row, a power of two and
-// the sum of exponentials of its part of the vocabulary relative to it; a
-// second kernel joins them and takes the targets' logits, as dot products of
-// their own.  The 4 N V bytes of logits are never written.
+// the sum of exponentials of its part of the vocabulary relative to it, and the logits of the
+// targets in it; a second kernel joins them.  The 4 N V bytes of logits are
+// never written.  A teacher's entries have a kernel of their own.
 //
 // Backward: the logits are computed again, a piece of the vocabulary at a
 // time (as much as the workspace takes), and softmax(z) goes to the
 // workspace twice: by rows (P, the factor of dx) and by vocabulary (Q, the
-// factor of dw, with the row's g); the few entries with a target are then
-// replaced by softmax(z) - q.  Two more products make the gradients.
+// factor of dw, with the row's g), less 1 at the targets; a teacher's
+// entries are replaced by softmax(z) - q afterwards.  Two more products make
+// the gradients.
 // dx of bf16 and fp16 is rounded to 16 bits at the end, so P is of that
 // type: its rounding errors are independent from entry to entry and stay
 // below that last rounding.  dw is fp32 (what a worker pushes), so Q is two fp16
@@ -57,10 +58,6 @@ __device__ __forceinline__ int index_of(const Targets& t, int64_t row, int k) {
     if (!t.target) return t.index[row * t.top + k];
     const int64_t v = t.target[row];
     return v >= 0 && v < t.vocab ? int(v) : -1;
-}
-
-__device__ __forceinline__ float weight_of(const Targets& t, int64_t row, int k) {
-    return t.target ? 1.0f : t.weight[row * t.top + k];
 }
 
 // A wave a row.  entropy: sum of q log q.
@@ -232,75 +229,15 @@ __global__ __launch_bounds__(256) void pack_rows(const T* src, int64_t stride, i
     if (largest) leave_largest(most, largest);
 }
 
-// Dot product of a row of x and a row of w, in every lane of the wave.
-template <typename T>
-__device__ __forceinline__ float row_dot(const T* x, const T* w, int cols) {
-    constexpr int E = kPerLoad<T>;
-    float s = 0.0f;
-#pragma unroll 4
-    for (int c = (int(threadIdx.x) & 63) * E; c < cols; c += 64 * E) {
-        const Piece<T> a = load_piece<T>(x + c, cols - c), b = load_piece<T>(w + c, cols - c);
-#pragma unroll
-        for (int e = 0; e < E; ++e) s = __builtin_fmaf(float(a.e[e]), float(b.e[e]), s);
-    }
-    return wave_sum(s);
-}
-
-// The logits of a teacher's entries: products of gathered rows of w, read
-// from memory or the caches once for each entry.  A wave takes four entries of a row,
-// so that four rows of w are in flight and x is read once for them.
-constexpr int kEntries = 4;
-
-template <typename T>
-__global__ __launch_bounds__(256) void target_logits(const T* x, int64_t x_stride, const T* w,
-                                                     int64_t w_stride, int64_t rows, int cols,
-                                                     Targets t, float inv_temperature, float* pick) {
-    constexpr int E = kPerLoad<T>;
-    const int groups = (t.top + kEntries - 1) / kEntries;
-    const int64_t unit = int64_t(blockIdx.x) * 4 + threadIdx.x / 64;
-    const int64_t row = unit / groups;
-    if (row >= rows) return;
-    const int first = int(unit % groups) * kEntries, lane = int(threadIdx.x) & 63;
-    int v[kEntries];
-    const T* wr[kEntries];
-    bool any = false;
-#pragma unroll
-    for (int k = 0; k < kEntries; ++k) {
-        v[k] = first + k < t.top ? t.index[row * t.top + first + k] : -1;
-        wr[k] = w + int64_t(max(v[k], 0)) * w_stride;
-        any |= v[k] >= 0;
-    }
-    if (!any) return;
-    const T* const xr = x + row * x_stride;
-    float s[kEntries] = {};
-#pragma unroll 2
-    for (int c = lane * E; c < cols; c += 64 * E) {
-        const Piece<T> a = load_piece<T>(xr + c, cols - c);
-        Piece<T> b[kEntries];
-#pragma unroll
-        for (int k = 0; k < kEntries; ++k) b[k] = load_piece<T>(wr[k] + c, cols - c);
-#pragma unroll
-        for (int k = 0; k < kEntries; ++k)
-#pragma unroll
-            for (int e = 0; e < E; ++e) s[k] = __builtin_fmaf(float(a.e[e]), float(b[k].e[e]), s[k]);
-    }
-#pragma unroll
-    for (int k = 0; k < kEntries; ++k) {
-        const float z = wave_sum(s[k]) * inv_temperature;
-        if (lane == 0 && v[k] >= 0) pick[row * t.top + first + k] = z;
-    }
-}
-
 // What the backward pass needs of each row: whether it has a target (alive: all bits
-// or none), its factor g T, its target's logit, the exponent of x and the
-// block's largest of factor x.  A wave a row at a time.
+// or none), its factor g T, the exponent of x and the block's largest of factor x.  A
+// wave a row at a time.
 template <typename T>
-__global__ __launch_bounds__(256) void prepare_rows(const T* x, int64_t x_stride, const T* w,
-                                                    int64_t w_stride, int64_t rows, int cols,
-                                                    Targets t, const int* teacher_alive,
+__global__ __launch_bounds__(256) void prepare_rows(const T* x, int64_t x_stride, int64_t rows,
+                                                    int cols, Targets t, const int* teacher_alive,
                                                     const float* dloss, float temperature,
-                                                    int* alive, float* factor, float* pick,
-                                                    int* row_exponent, int* largest) {
+                                                    int* alive, float* factor, int* row_exponent,
+                                                    int* largest) {
     const int lane = int(threadIdx.x) & 63;
     int most = kNoExponent;
     for (int64_t row = int64_t(blockIdx.x) * 4 + threadIdx.x / 64; row < rows;
@@ -317,10 +254,6 @@ __global__ __launch_bounds__(256) void prepare_rows(const T* x, int64_t x_stride
         const float size = __builtin_fabsf(f);
         if (size > 0.0f && size < __builtin_huge_valf())
             most = max(most, e + __builtin_amdgcn_frexp_expf(size));
-        if (live && t.target) {
-            const float z = row_dot<T>(xr, w + t.target[row] * w_stride, cols);
-            if (lane == 0) pick[row] = z;
-        }
     }
     leave_largest(most, largest);
 }
@@ -376,13 +309,23 @@ __global__ __launch_bounds__(256) void transpose(const T* src, int64_t stride, i
 struct Logits {
     int rows, vocab;       // valid rows of x; valid rows of w in this piece
     float inv_temperature;
-    const float* scale_x;  // [rows]; null: 1 (16-bit types)
-    const float* scale_w;  // [piece]; null: 1
+    const float* scale_x;   // [rows]; null: 1 (16-bit types)
+    const float* scale_w;   // [piece]; null: 1
+    const int64_t* target;  // [rows]; null: a teacher's entries
+    int64_t first;          // the piece's first vocabulary row
 };
+
+// A row's target as a row of w in this piece, or -1.
+__device__ __forceinline__ int target_of(const Logits& l, int row) {
+    if (!l.target || row >= l.rows) return -1;
+    const int64_t v = l.target[row] - l.first;
+    return v >= 0 && v < l.vocab ? int(v) : -1;
+}
 
 struct ForwardOut {
     f32x2* part;  // [blocks of 32 WR vocabulary rows][rows]: an exponent n, sum of exp(z) 2^-n
     int first_block;
+    float* pick;  // [rows]: the targets' logits
 };
 
 // Four consecutive values, 1 where there are none (the products they scale are 0).
@@ -403,13 +346,19 @@ __global__ __launch_bounds__(kProductThreads) void logits_forward(Product p, Log
     __shared__ __attribute__((aligned(1024))) char lds[TileShape<WR, WC>::kStageBytes * STAGES];
     const Place at = place(p);
     if (!at.live) return;
-    f32x16 acc[WR][WC];
-    multiply<T, WR, WC, STAGES>(p, at, lds, acc);
-
     const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) / 64;
     const int half = lane >> 5;
     const int block = at.r * 2 + wave / 2, v0 = block * WR * 32;
     const int i0 = (at.c * 2 + wave % 2) * WC * 32;
+    int target[WC];  // among the wave's entries
+#pragma unroll
+    for (int j = 0; j < WC; ++j) {
+        const int v = target_of(l, i0 + j * 32 + (lane & 31)) - v0;
+        target[j] = v < WR * 32 ? v : -1;
+    }
+    f32x16 acc[WR][WC];
+    multiply<T, WR, WC, STAGES>(p, at, lds, acc);
+
     const float low = -__builtin_huge_valf();
     if (v0 >= l.vocab) return;
 #pragma unroll
@@ -425,6 +374,19 @@ __global__ __launch_bounds__(kProductThreads) void logits_forward(Product p, Log
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[i][j][g * 4 + e] *= sx * sw[e];
                 }
+        }
+        if (__any(target[j] >= 0)) {
+            float z = 0.0f;
+            bool mine = false;
+#pragma unroll
+            for (int i = 0; i < WR; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (target[j] == i * 32 + r / 4 * 8 + half * 4 + r % 4) {
+                        z = acc[i][j][r];
+                        mine = true;
+                    }
+            if (mine) out.pick[row] = z;
         }
         f32x2 part;
         auto reduce = [&](auto is_cut) {
@@ -462,15 +424,82 @@ __global__ __launch_bounds__(kProductThreads) void logits_forward(Product p, Log
     }
 }
 
+// The logits of a teacher's entries, as the products above compute them: PAIRS (row,
+// entry) pairs a wave, rows of w gathered, of which the matrix instructions' 32 x 32
+// results give the diagonal.  The same instructions over the same k in the
+// same order give the same bits, and that matters: where softmax is near 1, an
+// error of the entry's logit that lse does not share stays whole in
+// softmax - q (with dot products of their own, fp32 gradients were 4e-6 off
+// instead of 1e-6).  Fragments come straight from memory, as no two pairs share
+// rows of w, those of the next kAhead instructions while this many are done.
+template <typename T, int PAIRS>
+__global__ __launch_bounds__(256) void target_logits(Operand x, Operand w, int k, int segments,
+                                                     Targets t, Logits l, float* pick) {
+    typedef typename Frag<T>::type F;
+    constexpr int kAhead = 8;
+    const int lane = int(threadIdx.x) & 63, n = lane & 31, half = lane >> 5;
+    const int64_t pair = (int64_t(blockIdx.x) * 4 + threadIdx.x / 64) * PAIRS + n;
+    const int64_t row = pair / t.top;
+    int64_t v = -1;
+    if (n < PAIRS && row < l.rows) v = t.index[pair] - l.first;
+    const bool in = v >= 0 && v < l.vocab;
+    if (!__any(in)) return;
+    const T* const xr = static_cast<const T*>(x.base) + (in ? row : 0) * x.ld + half * 8;
+    const T* const wr = static_cast<const T*>(w.base) + (in ? v : 0) * w.ld + half * 8;
+    struct Ahead {
+        F x[kAhead], w[kAhead];
+    };
+    // one past the end of the segments' loops is loaded as zeros
+    int seg = 0, at = 0;
+    auto fetch = [&](Ahead& f) {
+        const T* const xs = xr + (seg == 1 ? x.plane : 0) + at;  // planes as of (R, C) = (w, x)
+        const T* const ws = wr + (seg == 2 ? w.plane : 0) + at;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            f.x[u] = f.w[u] = F{};
+            if (in && seg < segments && at + u * 16 + half * 8 < k) {
+                f.x[u] = *reinterpret_cast<const F*>(xs + u * 16);
+                f.w[u] = *reinterpret_cast<const F*>(ws + u * 16);
+            }
+        }
+        at += 16 * kAhead;
+        if (at >= k) {
+            at = 0;
+            ++seg;
+        }
+    };
+    f32x16 acc{};
+    auto add = [&](const Ahead& f) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) acc = mfma(f.w[u], f.x[u], acc);
+    };
+    Ahead f0, f1;
+    fetch(f0);
+    while (true) {
+        const bool more = seg < segments;
+        fetch(f1);
+        add(f0);
+        if (!more) break;
+        const bool again = seg < segments;
+        fetch(f0);
+        add(f1);
+        if (!again) break;
+    }
+    // row n of column n: register n / 8 * 4 + n % 4 of the half wave n / 4 % 2
+    float z = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z = (n >> 3) * 4 + (n & 3) == r ? acc[r] : z;
+    if (!in || half != (n >> 2 & 1)) return;
+    const float sx = l.inv_temperature * (l.scale_x ? l.scale_x[row] : 1.0f);
+    pick[pair] = z * (sx * (l.scale_w ? l.scale_w[v] : 1.0f));
+}
+
 constexpr int kFinishRows = 16;
 
-// Joins the tiles' sums and takes the targets' logits: 16 rows a block,
-// their sums dealt to 64 groups of threads, the rows then to the waves.
-template <typename T>
+// Joins the tiles' sums: 16 rows a block, their sums dealt to 64 groups of
+// threads, the rows' targets then to the waves.
 __global__ __launch_bounds__(1024) void finish_loss(const f32x2* part, int blocks, int64_t rows,
-                                                    const T* x, int64_t x_stride, const T* w,
-                                                    int64_t w_stride, int cols, Targets t,
-                                                    const float* pick, const int* alive,
+                                                    Targets t, const float* pick, const int* alive,
                                                     const float* entropy, float temperature,
                                                     float* loss, float* lse) {
     __shared__ f32x2 words[64][kFinishRows];
@@ -510,8 +539,7 @@ __global__ __launch_bounds__(1024) void finish_loss(const f32x2* part, int block
     const float end = ends[wave];
     float out = 0.0f;
     if (t.target) {
-        const int v = index_of(t, row, 0);
-        if (v >= 0) out = end - row_dot<T>(x + row * x_stride, w + int64_t(v) * w_stride, cols);
+        if (index_of(t, row, 0) >= 0) out = end - pick[row];
     } else if (alive[row]) {
         for (int k = lane; k < t.top; k += 64) {
             const float q = t.weight[row * t.top + k];  // 0 where there is no entry
@@ -574,34 +602,49 @@ template <typename T, int PLANES, bool BOTH, int WR, int WC, int STAGES>
 __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Logits l,
                                                                    BackwardOut out) {
     // a wave's part of LDS: what it needs of its rows, then 32 WR x 32 WC entries of 16 bits
-    constexpr int kAbout = WR * 32 * 16, kPart = kAbout + WR * WC * 2048;
+    constexpr int kAbout = WR * 32 * 20, kPart = kAbout + WR * WC * 2048;
     constexpr int kStageBytes = TileShape<WR, WC>::kStageBytes * STAGES;
     __shared__ __attribute__((aligned(1024))) char lds[kStageBytes > 4 * kPart ? kStageBytes : 4 * kPart];
     const Place at = place(p);
     if (!at.live) return;
-    f32x16 acc[WR][WC];
-    multiply<T, WR, WC, STAGES>(p, at, lds, acc);
-
     const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) / 64;
     const int half = lane >> 5, odd = lane & 1;
     const int i0 = (at.r * 2 + wave / 2) * WR * 32, v0 = (at.c * 2 + wave % 2) * WC * 32;
     const bool want_p = BOTH || out.p, want_q = BOTH || out.q;
     const int largest = want_q ? largest_of(out.largest) : 0;
     const int largest_w = PLANES == 2 ? largest_of(out.largest_w) : 0;
-    // lse, scale, factor of Q, whether it is alive
-    f32x4* const about = reinterpret_cast<f32x4*>(lds + wave * kPart);
-    for (int r = lane; r < WR * 32; r += 64) {
-        const int row = i0 + r;
-        f32x4 a = {};
-        if (row < l.rows) {
-            a.x = out.lse[row];
-            a.y = l.inv_temperature * (PLANES == 2 ? l.scale_x[row] : 1.0f);
+    // the wave's rows, one or two a lane: lse, scale, factor of Q, whether it is
+    // alive; and its target among the wave's entries
+    constexpr int kMine = (WR * 32 + 63) / 64;
+    f32x4 mine[kMine];
+    int target[kMine];
+#pragma unroll
+    for (int u = 0; u < kMine; ++u) {
+        const int row = i0 + u * 64 + lane;
+        const bool have = u * 64 + lane < WR * 32 && row < l.rows;
+        mine[u] = f32x4{};
+        if (have) {
+            mine[u].x = out.lse[row];
+            mine[u].y = l.inv_temperature * (PLANES == 2 ? l.scale_x[row] : 1.0f);
             if (want_q)
-                a.z = __builtin_amdgcn_ldexpf(out.factor[row], out.row_exponent[row] - largest + 14);
-            a.w = __builtin_bit_cast(float, out.alive[row]);
+                mine[u].z =
+                    __builtin_amdgcn_ldexpf(out.factor[row], out.row_exponent[row] - largest + 14);
+            mine[u].w = __builtin_bit_cast(float, out.alive[row]);
         }
-        about[r] = a;
+        const int v = have ? target_of(l, row) - v0 : -1;
+        target[u] = v < WC * 32 ? v : -1;
     }
+    f32x16 acc[WR][WC];
+    multiply<T, WR, WC, STAGES>(p, at, lds, acc);
+
+    f32x4* const about = reinterpret_cast<f32x4*>(lds + wave * kPart);
+    int* const targets = reinterpret_cast<int*>(about + WR * 32);
+#pragma unroll
+    for (int u = 0; u < kMine; ++u)
+        if (u * 64 + lane < WR * 32) {
+            about[u * 64 + lane] = mine[u];
+            targets[u * 64 + lane] = target[u];
+        }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // other lanes of the wave read them
     float sw[WC], cw[WC];
     uint32_t in[WC];
@@ -646,6 +689,9 @@ __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Lo
             f32x4 row[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) row[e] = about[i * 32 + g * 8 + half * 4 + e];
+            typedef int i32x4 __attribute__((ext_vector_type(4)));
+            const i32x4 hit = *reinterpret_cast<const i32x4*>(targets + i * 32 + g * 8 + half * 4);
+            const bool any = __any(max(max(hit.x, hit.y), max(hit.z, hit.w)) >= 0);
 #pragma unroll
             for (int j = 0; j < WC; ++j) {
                 f32x4 y;
@@ -659,6 +705,10 @@ __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Lo
                     y[e] = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, s) &
                                                          __builtin_bit_cast(uint32_t, mask) & in[j]);
                 }
+                if (any)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        y[e] -= hit[e] == j * 32 + (lane & 31) ? 1.0f : 0.0f;
                 if (want_p) {
                     f32x4 c;
 #pragma unroll
@@ -740,7 +790,7 @@ __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Lo
     }
 }
 
-// The entries of P and Q with a target, a thread each: softmax - q.
+// The entries of P and Q that a teacher has too, a thread each: softmax - q.
 template <typename T, int PLANES>
 __global__ __launch_bounds__(256) void take_targets(Targets t, int64_t rows, int first, int vocab,
                                                     const float* pick, const float* scale_w,
@@ -750,10 +800,9 @@ __global__ __launch_bounds__(256) void take_targets(Targets t, int64_t rows, int
     const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x;
     const int64_t row = at / t.top;
     if (row >= rows) return;
-    const int k = int(at % t.top);
-    const int v = index_of(t, row, k) - first;
+    const int v = t.index[at] - first;
     if (v < 0 || v >= vocab) return;
-    const float s = __builtin_amdgcn_exp2f((pick[at] - out.lse[row]) * kLog2e) - weight_of(t, row, k);
+    const float s = __builtin_amdgcn_exp2f((pick[at] - out.lse[row]) * kLog2e) - t.weight[at];
     if (out.p) {
         const float c = PLANES == 2                       ? __builtin_amdgcn_ldexpf(scale_w[v], 28 - largest_w)
                         : std::is_same<T, fp16>::value ? 16384.0f
@@ -1078,7 +1127,7 @@ Layout lay_out(const VocabArgs& a, bool grad, int64_t piece, Arena* arena) {
     l.part = arena->take<f32x2>((a.vocab / (kTileRows[l.shape] / 2) + l.pieces) * a.rows, !grad);
     l.alive = arena->take<int>(a.rows, grad);
     l.factor = arena->take<float>(a.rows, grad);
-    l.pick = arena->take<float>(entries, grad || a.top > 0);
+    l.pick = arena->take<float>(entries, !grad || a.top > 0);
     l.row_exponent = arena->take<int>(a.rows, grad);
     l.largest = arena->take<int>(kExponentBlocks, grad);
     l.scale_x = arena->take<float>(a.rows, a.type == kF32);
@@ -1130,17 +1179,11 @@ Targets targets_of(const VocabArgs& a, const Layout& l) {
     return {std::max(1, a.top), int(a.vocab), a.top ? nullptr : a.target, l.index, l.weight};
 }
 
-// A teacher's distribution and its entries' logits.
-template <typename S>
 hipError_t teacher_of(const VocabArgs& a, const Layout& l, hipStream_t stream) {
     if (a.top == 0) return hipSuccess;
     hipLaunchKernelGGL(prepare_teacher, dim3(unsigned((a.rows + 3) / 4)), dim3(256),
                        unsigned(a.top) * 32, stream, a.rows, a.vocab, a.top, a.target, a.logit,
                        a.temperature, l.index, l.weight, l.teacher_alive, l.entropy);
-    const int64_t waves = a.rows * ((a.top + kEntries - 1) / kEntries);
-    hipLaunchKernelGGL(target_logits<S>, dim3(unsigned((waves + 3) / 4)), dim3(256), 0, stream,
-                       static_cast<const S*>(a.x), a.x_stride, static_cast<const S*>(a.w), a.w_stride,
-                       a.rows, int(a.cols), targets_of(a, l), 1.0f / a.temperature, l.pick);
     return hipGetLastError();
 }
 
@@ -1204,14 +1247,31 @@ hipError_t logits_of(const VocabArgs& a, const Layout& l, int64_t i, Operand* x,
         *x = {a.x, a.x_stride, 0, int(a.rows)};
     p->k = int(up(a.cols, 8));
     p->segments = l.planes == 2 ? 3 : 1;
-    *z = {int(a.rows), int(at.rows), 1.0f / a.temperature, l.scale_x, l.scale_w};
+    *z = {int(a.rows), int(at.rows), 1.0f / a.temperature, l.scale_x, l.scale_w,
+          a.top ? nullptr : a.target, at.first};
     return hipSuccess;
+}
+
+// The logits of a teacher's entries in a piece.  Few pairs are spread over more
+// waves.
+template <typename T>
+hipError_t pick_of(const VocabArgs& a, const Layout& l, const Operand& x, const Operand& w,
+                   const Product& p, const Logits& z, hipStream_t stream) {
+    if (a.top == 0) return hipSuccess;
+    const int64_t pairs = a.rows * a.top;
+    if (pairs < 4 * kUnits * 32)
+        hipLaunchKernelGGL((target_logits<T, 8>), dim3(unsigned((pairs + 31) / 32)), dim3(256), 0,
+                           stream, x, w, p.k, p.segments, targets_of(a, l), z, l.pick);
+    else
+        hipLaunchKernelGGL((target_logits<T, 32>), dim3(unsigned((pairs + 127) / 128)), dim3(256), 0,
+                           stream, x, w, p.k, p.segments, targets_of(a, l), z, l.pick);
+    return hipGetLastError();
 }
 
 // S: element type of x and w; T: of the products of logits and dx.
 template <typename S, typename T>
 hipError_t loss_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
-    hipError_t e = teacher_of<S>(a, l, stream);
+    hipError_t e = teacher_of(a, l, stream);
     if (e == hipSuccess) e = pack_x<S>(a, l, stream);
     int blocks = 0;
     for (int64_t i = 0; i < l.pieces && e == hipSuccess; ++i) {
@@ -1219,21 +1279,20 @@ hipError_t loss_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
         Logits z;
         e = logits_of<S>(a, l, i, &p.c, &p.r, &p, &z, stream);
         if (e != hipSuccess) break;
-        const ForwardOut o{l.part, blocks};
+        const ForwardOut o{l.part, blocks, l.pick};
         if constexpr (std::is_same<S, float>::value)
             e = run_forward<T, true>(l.shape, p, z, o, stream);
         else
             e = a.temperature == 1.0f ? run_forward<T, false>(l.shape, p, z, o, stream)
                                       : run_forward<T, true>(l.shape, p, z, o, stream);
+        if (e == hipSuccess) e = pick_of<T>(a, l, p.c, p.r, p, z, stream);
         const int block = kTileRows[l.shape] / 2;
         blocks += (z.vocab + block - 1) / block;
     }
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(finish_loss<S>, dim3(unsigned((a.rows + kFinishRows - 1) / kFinishRows)),
-                       dim3(1024), 0, stream, l.part, blocks, a.rows, static_cast<const S*>(a.x),
-                       a.x_stride, static_cast<const S*>(a.w), a.w_stride, int(a.cols),
-                       targets_of(a, l), l.pick, l.teacher_alive, l.entropy, a.temperature, a.loss,
-                       a.lse);
+    hipLaunchKernelGGL(finish_loss, dim3(unsigned((a.rows + kFinishRows - 1) / kFinishRows)),
+                       dim3(1024), 0, stream, l.part, blocks, a.rows, targets_of(a, l), l.pick,
+                       l.teacher_alive, l.entropy, a.temperature, a.loss, a.lse);
     return hipGetLastError();
 }
 
@@ -1242,13 +1301,13 @@ hipError_t grad_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
     constexpr int PLANES = std::is_same<S, float>::value ? 2 : 1;
     const Targets targets = targets_of(a, l);
     const Largest largest{l.largest, row_blocks(a.rows)};
-    hipError_t e = teacher_of<S>(a, l, stream);
+    hipError_t e = teacher_of(a, l, stream);
     if (e == hipSuccess) e = pack_x<S>(a, l, stream);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(prepare_rows<S>, dim3(unsigned(row_blocks(a.rows))), dim3(256), 0, stream,
-                       static_cast<const S*>(a.x), a.x_stride, static_cast<const S*>(a.w),
-                       a.w_stride, a.rows, int(a.cols), targets, l.teacher_alive, a.dloss,
-                       a.temperature, l.alive, l.factor, l.pick, l.row_exponent, l.largest);
+                       static_cast<const S*>(a.x), a.x_stride, a.rows, int(a.cols), targets,
+                       l.teacher_alive, a.dloss, a.temperature, l.alive, l.factor, l.row_exponent,
+                       l.largest);
     if (a.dw) {
         const dim3 by_tile(unsigned(up(a.rows, 64) / 64), unsigned((a.cols + 63) / 64));
         hipLaunchKernelGGL((transpose<S, true>), by_tile, dim3(256), 0, stream,
@@ -1268,10 +1327,14 @@ hipError_t grad_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
         e = a.dx && a.dw ? run_backward<T, PLANES, true>(l.shape, p, z, o, stream)
                          : run_backward<T, PLANES, false>(l.shape, p, z, o, stream);
         if (e != hipSuccess) return e;
-        const int64_t entries = a.rows * targets.top;
-        hipLaunchKernelGGL((take_targets<T, PLANES>), dim3(unsigned((entries + 255) / 256)), dim3(256),
-                           0, stream, targets, a.rows, int(at.first), int(at.rows), l.pick,
-                           l.scale_w, o);
+        if ((e = pick_of<T>(a, l, p.r, p.c, p, z, stream)) != hipSuccess) return e;
+        if (a.top) {
+            const int64_t entries = a.rows * a.top;
+            hipLaunchKernelGGL((take_targets<T, PLANES>), dim3(unsigned((entries + 255) / 256)),
+                               dim3(256), 0, stream, targets, a.rows, int(at.first), int(at.rows),
+                               l.pick, l.scale_w, o);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+        }
         if (a.dx) {
             const int64_t k = up(at.rows, 64);
             const S* const w = static_cast<const S*>(a.w) + at.first * a.w_stride;
