@@ -126,10 +126,11 @@ __device__ __forceinline__ void arrive() {
 }
 
 // The product of one tile: acc[i][j] is the wave's 32 x 32 block i along R, j
-// along C.  On return LDS is free.
-template <typename T, int WR, int WC, int STAGES>
+// along C.  `meanwhile` is called while the first loads are on their way.  On
+// return LDS is free.
+template <typename T, int WR, int WC, int STAGES, typename M>
 __device__ __forceinline__ void multiply(const Product& p, const Place& at, char* lds,
-                                         f32x16 (&acc)[WR][WC]) {
+                                         f32x16 (&acc)[WR][WC], M meanwhile) {
     typedef TileShape<WR, WC> S;
     typedef typename Frag<T>::type F;
     constexpr int LR = S::kR * S::kRowBytes / 4096;  // loads of a wave that are R's
@@ -255,6 +256,7 @@ __device__ __forceinline__ void multiply(const Product& p, const Place& at, char
 #pragma unroll
             for (int j = 0; j < S::kLoads; ++j) load(j);
     }
+    meanwhile();
     arrive<(STAGES - 2) * S::kLoads>();
     Frags f0, f1;
 #pragma unroll

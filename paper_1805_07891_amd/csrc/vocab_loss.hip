@@ -143,24 +143,38 @@ __device__ __forceinline__ void split(float v, int e, fp16* high, fp16* low) {
     *low = fp16(s - float(*high));
 }
 
+// Eight whole pieces of a row, the first of them number `first`, in flight at
+// once; past the row's last whole piece that one again.
+constexpr int kBatch = 8;
+
 template <typename T>
-__device__ __forceinline__ float row_largest(const T* p, int cols) {
-    constexpr int E = kPerLoad<T>;
+__device__ __forceinline__ void load_batch(const T* p, int first, int whole, Piece<T> (&r)[kBatch]) {
     const int lane = int(threadIdx.x) & 63;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+        __builtin_memcpy(&r[u], p + min(first + u * 64 + lane, whole - 1) * kPerLoad<T>, 16);
+}
+
+__device__ __forceinline__ float larger(float most, float v) {
+    v = __builtin_fabsf(v);
+    return v > most || v != v ? v : most;
+}
+
+// The largest magnitude of a row (NaN if it holds one), and its last batch.
+template <typename T>
+__device__ __forceinline__ float row_largest(const T* p, int cols, Piece<T> (&r)[kBatch]) {
+    const int whole = cols / kPerLoad<T>;
     float most = 0.0f;
-    for (int c = lane * E; c < cols; c += 64 * E) {
-        const Piece<T> r = load_piece<T>(p + c, cols - c);
+    for (int first = 0; first < whole; first += 64 * kBatch) {
+        load_batch(p, first, whole, r);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float v = __builtin_fabsf(float(r.e[e]));
-            most = v > most || v != v ? v : most;
-        }
-    }
+        for (int u = 0; u < kBatch; ++u)
 #pragma unroll
-    for (int d = 32; d; d >>= 1) {
-        const float o = __shfl_xor(most, d);
-        most = o > most || o != o ? o : most;
+            for (int e = 0; e < kPerLoad<T>; ++e) most = larger(most, float(r[u].e[e]));
     }
+    for (int c = whole * kPerLoad<T>; c < cols; ++c) most = larger(most, float(p[c]));
+#pragma unroll
+    for (int d = 32; d; d >>= 1) most = larger(most, __shfl_xor(most, d));
     return most;
 }
 
@@ -202,27 +216,56 @@ __global__ __launch_bounds__(256) void pack_rows(const T* src, int64_t stride, i
     for (int64_t row = int64_t(blockIdx.x) * 4 + threadIdx.x / 64; row < rows;
          row += int64_t(gridDim.x) * 4) {
         const T* const p = src + row * stride;
+        const int whole = cols / E;
+        int e = 0;
         if constexpr (std::is_same<T, float>::value) {
-            const int e = exponent_of(row_largest<T>(p, cols));
+            Piece<T> r[kBatch];
+            e = exponent_of(row_largest<T>(p, cols, r));
             most = max(most, e);
             if (lane == 0) {
                 scale[row] = __builtin_amdgcn_ldexpf(1.0f, e - 14);
                 if (row_exponent) row_exponent[row] = e;
             }
-            fp16* const out = static_cast<fp16*>(dst) + row * ld;
-            for (int c = lane * E; c < ld; c += 64 * E) {
-                const Piece<T> r = load_piece<T>(p + c, cols - c);
-                fp16 h[E], l[E];
+            for (int first = 0; first < whole; first += 64 * kBatch) {
+                // (a row of one batch is in registers already)
+                if (whole > 64 * kBatch) load_batch(p, first, whole, r);
 #pragma unroll
-                for (int i = 0; i < E; ++i) split(r.e[i], e, h + i, l + i);
-                __builtin_memcpy(out + c, h, sizeof h);
-                __builtin_memcpy(out + plane + c, l, sizeof l);
+                for (int u = 0; u < kBatch; ++u) {
+                    const int i = first + u * 64 + lane;
+                    fp16 h[E], l[E];
+#pragma unroll
+                    for (int k = 0; k < E; ++k) split(r[u].e[k], e, h + k, l + k);
+                    fp16* const to = static_cast<fp16*>(dst) + row * ld + i * E;
+                    if (i < whole) {
+                        __builtin_memcpy(__builtin_assume_aligned(to, 8), h, sizeof h);
+                        __builtin_memcpy(__builtin_assume_aligned(to + plane, 8), l, sizeof l);
+                    }
+                }
             }
         } else {
-            T* const out = static_cast<T*>(dst) + row * ld;
-            for (int c = lane * E; c < ld; c += 64 * E) {
-                const Piece<T> r = load_piece<T>(p + c, cols - c);
-                __builtin_memcpy(out + c, &r, 16);
+            typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+            for (int first = 0; first < whole; first += 64 * kBatch) {
+                u32x4 r[kBatch];
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u)
+                    __builtin_memcpy(&r[u], p + min(first + u * 64 + lane, whole - 1) * E, 16);
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) {
+                    const int i = first + u * 64 + lane;
+                    if (i < whole) *reinterpret_cast<u32x4*>(static_cast<T*>(dst) + row * ld + i * E) = r[u];
+                }
+            }
+        }
+        // the columns behind the last whole piece, and zeros
+        for (int c = whole * E + lane; c < ld; c += 64) {
+            const T v = c < cols ? p[c] : T(0.0f);
+            if constexpr (std::is_same<T, float>::value) {
+                fp16 h, l;
+                split(v, e, &h, &l);
+                static_cast<fp16*>(dst)[row * ld + c] = h;
+                static_cast<fp16*>(dst)[plane + row * ld + c] = l;
+            } else {
+                static_cast<T*>(dst)[row * ld + c] = v;
             }
         }
     }
@@ -245,7 +288,8 @@ __global__ __launch_bounds__(256) void prepare_rows(const T* x, int64_t x_stride
         const T* const xr = x + row * x_stride;
         const bool live = teacher_alive ? teacher_alive[row] != 0 : index_of(t, row, 0) >= 0;
         const float f = !live ? 0.0f : (dloss ? dloss[row] : 1.0f) * temperature;
-        const int e = exponent_of(row_largest<T>(xr, cols));
+        Piece<T> r[kBatch];
+        const int e = exponent_of(row_largest<T>(xr, cols, r));
         if (lane == 0) {
             alive[row] = live ? -1 : 0;
             factor[row] = f;
@@ -328,19 +372,13 @@ struct ForwardOut {
     float* pick;  // [rows]: the targets' logits
 };
 
-// Four consecutive values, 1 where there are none (the products they scale are 0).
-__device__ __forceinline__ f32x4 four(const float* p, int at, int end) {
-    f32x4 s = {1.0f, 1.0f, 1.0f, 1.0f};
-    if (p)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (at + e < end) s[e] = p[at + e];
-    return s;
-}
+// How logits come from the product: as they are; by the temperature; and, of
+// fp32 types, by the rows' scales too.
+enum Scaling { kPlain = 0, kTemperature = 1, kScaledRows = 2 };
 
 // R is w, C is x: a lane has one row of x and, in registers, entries of the
-// vocabulary.  SCALED: fp32's rows, and temperatures other than 1.
-template <typename T, bool SCALED, int WR, int WC, int STAGES>
+// vocabulary.
+template <typename T, int SCALING, int WR, int WC, int STAGES>
 __global__ __launch_bounds__(kProductThreads) void logits_forward(Product p, Logits l,
                                                                   ForwardOut out) {
     __shared__ __attribute__((aligned(1024))) char lds[TileShape<WR, WC>::kStageBytes * STAGES];
@@ -351,30 +389,37 @@ __global__ __launch_bounds__(kProductThreads) void logits_forward(Product p, Log
     const int block = at.r * 2 + wave / 2, v0 = block * WR * 32;
     const int i0 = (at.c * 2 + wave % 2) * WC * 32;
     int target[WC];  // among the wave's entries
-#pragma unroll
-    for (int j = 0; j < WC; ++j) {
-        const int v = target_of(l, i0 + j * 32 + (lane & 31)) - v0;
-        target[j] = v < WR * 32 ? v : -1;
-    }
+    float sx[WC];
+    f32x4 sw[WR][4];
     f32x16 acc[WR][WC];
-    multiply<T, WR, WC, STAGES>(p, at, lds, acc);
+    multiply<T, WR, WC, STAGES>(p, at, lds, acc, [&] {
+#pragma unroll
+        for (int j = 0; j < WC; ++j) {
+            const int row = i0 + j * 32 + (lane & 31), v = target_of(l, row) - v0;
+            target[j] = v < WR * 32 ? v : -1;
+            sx[j] = l.inv_temperature;
+            if (SCALING == kScaledRows && row < l.rows) sx[j] *= l.scale_x[row];
+        }
+        // (the scales' array goes on to the end of a tile)
+        if constexpr (SCALING == kScaledRows)
+#pragma unroll
+            for (int i = 0; i < WR; ++i)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    sw[i][g] = *reinterpret_cast<const f32x4*>(l.scale_w + v0 + i * 32 + g * 8 + half * 4);
+    });
 
     const float low = -__builtin_huge_valf();
     if (v0 >= l.vocab) return;
 #pragma unroll
     for (int j = 0; j < WC; ++j) {
         const int row = i0 + j * 32 + (lane & 31);
-        if constexpr (SCALED) {
-            const float sx = l.inv_temperature * (l.scale_x && row < l.rows ? l.scale_x[row] : 1.0f);
+        if constexpr (SCALING != kPlain)
 #pragma unroll
             for (int i = 0; i < WR; ++i)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const f32x4 sw = four(l.scale_w, v0 + i * 32 + g * 8 + half * 4, l.vocab);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[i][j][g * 4 + e] *= sx * sw[e];
-                }
-        }
+                for (int r = 0; r < 16; ++r)
+                    acc[i][j][r] *= SCALING == kScaledRows ? sx[j] * sw[i][r / 4][r % 4] : sx[j];
         if (__any(target[j] >= 0)) {
             float z = 0.0f;
             bool mine = false;
@@ -596,9 +641,8 @@ __device__ __forceinline__ void split4(const f32x4& y, uint32_t (&high)[2], uint
 // row of 256 bytes): written from registers, in pieces of 16 and 64 bytes,
 // the kernel took 2754 us instead of REWRITE for 8192 rows, 4096 columns and 32768
 // entries (bf16), 1.6 GB written.  T: type of the product's operands and of P;
-// PLANES: of P.  BOTH: P and Q are wanted
-// (known without asking at every entry).
-template <typename T, int PLANES, bool BOTH, int WR, int WC, int STAGES>
+// PLANES: of P; WANT: P (1), Q (2) or both (3).
+template <typename T, int PLANES, int WANT, int WR, int WC, int STAGES>
 __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Logits l,
                                                                    BackwardOut out) {
     // a wave's part of LDS: what it needs of its rows, then 32 WR x 32 WC entries of 16 bits
@@ -610,32 +654,33 @@ __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Lo
     const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) / 64;
     const int half = lane >> 5, odd = lane & 1;
     const int i0 = (at.r * 2 + wave / 2) * WR * 32, v0 = (at.c * 2 + wave % 2) * WC * 32;
-    const bool want_p = BOTH || out.p, want_q = BOTH || out.q;
-    const int largest = want_q ? largest_of(out.largest) : 0;
-    const int largest_w = PLANES == 2 ? largest_of(out.largest_w) : 0;
+    constexpr bool want_p = WANT & 1, want_q = WANT & 2;
     // the wave's rows, one or two a lane: lse, scale, factor of Q, whether it is
     // alive; and its target among the wave's entries
     constexpr int kMine = (WR * 32 + 63) / 64;
     f32x4 mine[kMine];
-    int target[kMine];
-#pragma unroll
-    for (int u = 0; u < kMine; ++u) {
-        const int row = i0 + u * 64 + lane;
-        const bool have = u * 64 + lane < WR * 32 && row < l.rows;
-        mine[u] = f32x4{};
-        if (have) {
-            mine[u].x = out.lse[row];
-            mine[u].y = l.inv_temperature * (PLANES == 2 ? l.scale_x[row] : 1.0f);
-            if (want_q)
-                mine[u].z =
-                    __builtin_amdgcn_ldexpf(out.factor[row], out.row_exponent[row] - largest + 14);
-            mine[u].w = __builtin_bit_cast(float, out.alive[row]);
-        }
-        const int v = have ? target_of(l, row) - v0 : -1;
-        target[u] = v < WC * 32 ? v : -1;
-    }
+    int target[kMine], largest_w = 0;
     f32x16 acc[WR][WC];
-    multiply<T, WR, WC, STAGES>(p, at, lds, acc);
+    multiply<T, WR, WC, STAGES>(p, at, lds, acc, [&] {
+        const int largest = want_q ? largest_of(out.largest) : 0;
+        if (PLANES == 2) largest_w = largest_of(out.largest_w);
+#pragma unroll
+        for (int u = 0; u < kMine; ++u) {
+            const int row = i0 + u * 64 + lane;
+            const bool have = u * 64 + lane < WR * 32 && row < l.rows;
+            mine[u] = f32x4{};
+            if (have) {
+                mine[u].x = out.lse[row];
+                mine[u].y = l.inv_temperature * (PLANES == 2 ? l.scale_x[row] : 1.0f);
+                if (want_q)
+                    mine[u].z =
+                        __builtin_amdgcn_ldexpf(out.factor[row], out.row_exponent[row] - largest + 14);
+                mine[u].w = __builtin_bit_cast(float, out.alive[row]);
+            }
+            const int v = have ? target_of(l, row) - v0 : -1;
+            target[u] = v < WC * 32 ? v : -1;
+        }
+    });
 
     f32x4* const about = reinterpret_cast<f32x4*>(lds + wave * kPart);
     int* const targets = reinterpret_cast<int*>(about + WR * 32);
@@ -669,17 +714,18 @@ __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Lo
     auto write_p = [&](int from) {  // rows from .. from + kRowsP of the wave's
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         constexpr int kAtOnce = 64 / kPiecesP;
+        const int piece = lane % kPiecesP;
 #pragma unroll
-        for (int m = 0; m < PLANES; ++m)
+        for (int m = 0; m < PLANES; ++m) {
+            int row = i0 + from + lane / kPiecesP;
+            T* to = static_cast<T*>(out.p) + m * out.plane_p + int64_t(row) * out.ld_p + v0 + piece * 8;
 #pragma unroll
-            for (int t0 = 0; t0 < kRowsP; t0 += kAtOnce) {
-                const int t = t0 + lane / kPiecesP, piece = lane % kPiecesP;
-                const f32x4 v = *reinterpret_cast<const f32x4*>(part + m * kRowsP * kPiecesP * 16 +
-                                                                place_p(t, piece));
-                T* const to = static_cast<T*>(out.p) + m * out.plane_p +
-                              int64_t(i0 + from + t) * out.ld_p + v0 + piece * 8;
-                if (i0 + from + t < l.rows) *reinterpret_cast<f32x4*>(to) = v;
+            for (int t0 = 0; t0 < kRowsP; t0 += kAtOnce, row += kAtOnce, to += kAtOnce * out.ld_p) {
+                const f32x4 v = *reinterpret_cast<const f32x4*>(
+                    part + m * kRowsP * kPiecesP * 16 + place_p(t0 + lane / kPiecesP, piece));
+                if (row < l.rows) *reinterpret_cast<f32x4*>(to) = v;
             }
+        }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     };
 #pragma unroll
@@ -712,7 +758,8 @@ __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Lo
                 if (want_p) {
                     f32x4 c;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) c[e] = rounded(y[e] * cw[j]);
+                    for (int e = 0; e < 4; ++e)
+                        c[e] = std::is_same<T, bf16>::value ? y[e] : rounded(y[e] * cw[j]);
                     uint32_t planes[2][2];
                     split4<T>(c, planes[0], planes[1]);
                     // neighbouring lanes exchange rows: even ones take rows 0 and 1 of the
@@ -779,12 +826,13 @@ __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Lo
                 }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         constexpr int kAtOnce = 64 / kPiecesQ;
+        const int piece = lane % kPiecesQ;
+        fp16* to = out.q + m * out.plane_q + int64_t(v0 + lane / kPiecesQ) * out.ld_q + i0 + piece * 8;
+        if (i0 + piece * 8 < out.ld_q) {
 #pragma unroll
-        for (int t0 = 0; t0 < WC * 32; t0 += kAtOnce) {
-            const int v = t0 + lane / kPiecesQ, piece = lane % kPiecesQ;
-            const f32x4 y = *reinterpret_cast<const f32x4*>(part + place_q(v, piece));
-            fp16* const to = out.q + m * out.plane_q + int64_t(v0 + v) * out.ld_q + i0 + piece * 8;
-            if (i0 + piece * 8 < out.ld_q) *reinterpret_cast<f32x4*>(to) = y;
+            for (int t0 = 0; t0 < WC * 32; t0 += kAtOnce, to += kAtOnce * out.ld_q)
+                *reinterpret_cast<f32x4*>(to) =
+                    *reinterpret_cast<const f32x4*>(part + place_q(t0 + lane / kPiecesQ, piece));
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
@@ -861,7 +909,7 @@ __global__ __launch_bounds__(kProductThreads) void grad_rows(Product p, DxOut ou
     const Place at = place(p);
     if (!at.live) return;
     f32x16 acc[WR][WC];
-    multiply<T, WR, WC, STAGES>(p, at, lds, acc);
+    multiply<T, WR, WC, STAGES>(p, at, lds, acc, [] {});
 
     const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) / 64;
     const int c0 = (at.r * 2 + wave / 2) * WR * 32, i0 = (at.c * 2 + wave % 2) * WC * 32;
@@ -935,7 +983,7 @@ __global__ __launch_bounds__(kProductThreads) void grad_weights(Product p, DwOut
     const Place at = place(p);
     if (!at.live) return;
     f32x16 acc[WR][WC];
-    multiply<fp16, WR, WC, STAGES>(p, at, lds, acc);
+    multiply<fp16, WR, WC, STAGES>(p, at, lds, acc, [] {});
 
     const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) / 64;
     const int c0 = (at.r * 2 + wave / 2) * WR * 32, v0 = (at.c * 2 + wave % 2) * WC * 32;
@@ -1030,19 +1078,19 @@ hipError_t launch_product(K kernel, Product p, hipStream_t stream, const A&... a
     : (shape) == kMid ? call(2, 2, kStages[kMid])  \
                       : call(1, 1, kStages[kSmall])
 
-template <typename T, bool SCALED>
+template <typename T, int SCALING>
 hipError_t run_forward(int shape, const Product& p, const Logits& l, const ForwardOut& o,
                        hipStream_t stream) {
-#define PHUB_CALL(a, b, s) launch_product<a, b>(logits_forward<T, SCALED, a, b, s>, p, stream, l, o)
+#define PHUB_CALL(a, b, s) launch_product<a, b>(logits_forward<T, SCALING, a, b, s>, p, stream, l, o)
     return PHUB_BY_SHAPE(shape, PHUB_CALL);
 #undef PHUB_CALL
 }
 
-template <typename T, int PLANES, bool BOTH>
+template <typename T, int PLANES, int WANT>
 hipError_t run_backward(int shape, const Product& p, const Logits& l, const BackwardOut& o,
                         hipStream_t stream) {
 #define PHUB_CALL(a, b, s) \
-    launch_product<a, b>(logits_backward<T, PLANES, BOTH, a, b, s>, p, stream, l, o)
+    launch_product<a, b>(logits_backward<T, PLANES, WANT, a, b, s>, p, stream, l, o)
     return PHUB_BY_SHAPE(shape, PHUB_CALL);
 #undef PHUB_CALL
 }
@@ -1281,10 +1329,10 @@ hipError_t loss_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
         if (e != hipSuccess) break;
         const ForwardOut o{l.part, blocks, l.pick};
         if constexpr (std::is_same<S, float>::value)
-            e = run_forward<T, true>(l.shape, p, z, o, stream);
+            e = run_forward<T, kScaledRows>(l.shape, p, z, o, stream);
         else
-            e = a.temperature == 1.0f ? run_forward<T, false>(l.shape, p, z, o, stream)
-                                      : run_forward<T, true>(l.shape, p, z, o, stream);
+            e = a.temperature == 1.0f ? run_forward<T, kPlain>(l.shape, p, z, o, stream)
+                                      : run_forward<T, kTemperature>(l.shape, p, z, o, stream);
         if (e == hipSuccess) e = pick_of<T>(a, l, p.c, p.r, p, z, stream);
         const int block = kTileRows[l.shape] / 2;
         blocks += (z.vocab + block - 1) / block;
@@ -1324,8 +1372,9 @@ hipError_t grad_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
         if ((e = logits_of<S>(a, l, i, &p.r, &p.c, &p, &z, stream)) != hipSuccess) return e;
         const BackwardOut o{a.lse, l.alive, l.factor, l.row_exponent, largest, largest_w,
                             l.p, l.ld_p, a.rows * l.ld_p, l.q, l.rows_ld, l.piece * l.rows_ld};
-        e = a.dx && a.dw ? run_backward<T, PLANES, true>(l.shape, p, z, o, stream)
-                         : run_backward<T, PLANES, false>(l.shape, p, z, o, stream);
+        e = !a.dw   ? run_backward<T, PLANES, 1>(l.shape, p, z, o, stream)
+            : !a.dx ? run_backward<T, PLANES, 2>(l.shape, p, z, o, stream)
+                    : run_backward<T, PLANES, 3>(l.shape, p, z, o, stream);
         if (e != hipSuccess) return e;
         if ((e = pick_of<T>(a, l, p.r, p.c, p, z, stream)) != hipSuccess) return e;
         if (a.top) {

@@ -25,7 +25,9 @@ import torch
 _TYPES = {torch.float32: _phub.PHUB_F32, torch.bfloat16: _phub.PHUB_BF16,
           torch.float16: _phub.PHUB_F16}
 _FP32 = torch.float32
-_empty, _stream_of = torch.empty, torch._C._cuda_getCurrentRawStream
+# (the tensors are on a GPU already where these are called)
+_empty, _current_device = torch.empty, torch._C._cuda_getDevice
+_stream_of = torch._C._cuda_getCurrentRawStream
 _default = None
 
 
@@ -45,7 +47,9 @@ def _matrix(name, t, shape=None, dtype=None, device=None):
         raise ValueError(f"{name} must be 2-D with adjacent columns")
     if shape is not None and size != shape:
         raise ValueError(f"{name} has shape {tuple(size)}, expected {tuple(shape)}")
-    _same(name, t, dtype, device)
+    if (dtype is not None and t.dtype is not dtype) or not t.is_cuda or (
+            device is not None and t.device != device):
+        _wrong(name, t, dtype, device)
     # the stride of a matrix of one row says nothing
     return t.data_ptr(), (t.stride(0) if size[0] > 1 else size[1])
 
@@ -62,23 +66,24 @@ def _rows(x):
 def _vector(name, t, n, dtype, device):
     if t is None:
         return None
-    if len(t.shape) != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+    if t.dtype is not dtype or not t.is_cuda or t.device != device:
+        _wrong(name, t, dtype, device)
+    size = t.shape
+    if len(size) != 1 or size[0] != n or not t.is_contiguous():
         raise ValueError(f"{name} must be {n} adjacent values")
-    _same(name, t, dtype, device)
     return t.data_ptr()
 
 
-def _same(name, t, dtype, device):
-    if dtype is not None and t.dtype != dtype:
+def _wrong(name, t, dtype, device):
+    if dtype is not None and t.dtype is not dtype:
         raise ValueError(f"{name} is {t.dtype}, expected {dtype}")
-    if not t.is_cuda or (device is not None and t.device != device):
-        raise ValueError(f"{name} is on {t.device}, expected {device or 'a GPU'}")
+    raise ValueError(f"{name} is on {t.device}, expected {device or 'a GPU'}")
 
 
 def _call(device, function, *args):
     """function(*args, torch's current stream of the device), on the device."""
     index = device.index
-    before = torch.cuda.current_device()
+    before = _current_device()
     if before == index:
         return function(*args, _stream_of(index))
     torch.cuda.set_device(index)
@@ -102,7 +107,8 @@ def _workspace(workspace, device):
     """(pointer, bytes) of a workspace, checked."""
     if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous uint8 tensor")
-    _same("workspace", workspace, None, device)
+    if workspace.device != device:
+        _wrong("workspace", workspace, None, device)
     return workspace.data_ptr(), workspace.numel()
 
 
