@@ -501,9 +501,13 @@ int phub_vocab_bytes(int type, int64_t rows, int64_t cols, int64_t vocab, const 
  *             outside [0, vocab) (padding) has loss 0 and no gradient,
  *             whatever its hidden states hold.
  *   loss, lse receive a value for each row.
- * 0 <= rows <= 2^22, 1 <= cols <= 2^16, 1 <= vocab <= 2^24, strides at most
- * 2^22.  A vector of biases can be a column of w that meets a column of ones
+ * 0 <= rows <= 2^21, 1 <= cols <= 2^16, 1 <= vocab <= 2^24, strides at most
+ * 2^21.  A vector of biases can be a column of w that meets a column of ones
  * in x.
+ * Products of fp32 matrices are made of two 16-bit parts of each value: right
+ * to about 2^-23 of each product, and to 2^-38 of the largest values of the two rows
+ * where others are much smaller.  A value that is not finite makes the logits
+ * of its row (or, in w, of its entry) not finite.
  */
 int phub_vocab_loss(int type, int64_t rows, int64_t cols, int64_t vocab, const void *x,
                     int64_t x_stride, const void *w, int64_t w_stride, const int64_t *target,
@@ -534,8 +538,8 @@ int phub_vocab_loss_grad(int type, int64_t rows, int64_t cols, int64_t vocab, co
  *                 [0, vocab) or a logit of -infinity are absent; entries of
  *                 one row with the same index add up to one.  A row without
  *                 entries has loss 0 and no gradient.
- * 1 <= top <= 1024, T finite and > 0; other arguments and limits as
- * phub_vocab_loss.
+ * 1 <= top <= 1024, rows * top <= 2^30, 1e-6 <= T <= 1e6; other arguments and
+ * limits as phub_vocab_loss.
  */
 int phub_distill_loss(int type, int64_t rows, int64_t cols, int64_t vocab, const void *x,
                       int64_t x_stride, const void *w, int64_t w_stride, int top,

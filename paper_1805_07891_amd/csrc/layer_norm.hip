@@ -437,6 +437,22 @@ __global__ __launch_bounds__(256) void norm_clear(int64_t cols, float* dweight, 
     if (dbias) dbias[c] = 0.0f;
 }
 
+// Rows of one launch that has a block a row: a launch's threads are counted in 32
+// bits.
+constexpr int64_t kLaunchRows = int64_t(1) << 20;
+
+// The arguments of at most kLaunchRows rows from `row` on, without the sums.
+NormArgs rows_from(NormArgs a, int64_t row) {
+    const int64_t size = a.type == kF32 ? 4 : 2;
+    a.x = static_cast<const char*>(a.x) + row * a.x_stride * size;
+    if (a.dy) a.dy = static_cast<const char*>(a.dy) + row * a.dy_stride * size;
+    if (a.y) a.y = static_cast<char*>(a.y) + row * a.y_stride * size;
+    if (a.mean) a.mean += row;
+    if (a.rstd) a.rstd += row;
+    a.rows = std::min<int64_t>(a.rows - row, kLaunchRows);
+    return a;
+}
+
 template <typename T, int LANES, int PIECES>
 void launch_forward(const NormArgs& a, hipStream_t stream) {
     constexpr int THREADS = LANES < 256 ? 256 : LANES, ROWS = THREADS / LANES;
@@ -503,8 +519,11 @@ hipError_t backward(NormArgs a, hipStream_t stream) {
         launch_backward<T, 512, 32>(a, strips, stream);
     } else {
         const int64_t pieces = (a.cols + kPerLoad<T> - 1) / kPerLoad<T>;
-        if (a.y)
-            hipLaunchKernelGGL(norm_backward_long<T>, dim3(unsigned(a.rows)), dim3(1024), 0, stream, a);
+        for (int64_t row = 0; a.y && row < a.rows; row += kLaunchRows) {
+            const NormArgs part = rows_from(a, row);
+            hipLaunchKernelGGL(norm_backward_long<T>, dim3(unsigned(part.rows)), dim3(1024), 0, stream,
+                               part);
+        }
         if (a.partial)
             hipLaunchKernelGGL(norm_strip_sums<T>,
                                dim3(unsigned(strips), unsigned((pieces + 255) / 256)), dim3(256), 0,
@@ -522,10 +541,14 @@ hipError_t backward(NormArgs a, hipStream_t stream) {
 int64_t norm_strips(int64_t rows, int64_t) { return std::min<int64_t>(rows, kStripBlocks); }
 
 hipError_t launch_layer_norm(const NormArgs& a, hipStream_t stream) {
-    if (a.rows == 0) return hipSuccess;
-    return a.type == kF32    ? forward<float>(a, stream)
-           : a.type == kBf16 ? forward<bf16>(a, stream)
-                             : forward<fp16>(a, stream);
+    for (int64_t row = 0; row < a.rows; row += kLaunchRows) {
+        const NormArgs part = rows_from(a, row);
+        const hipError_t e = a.type == kF32    ? forward<float>(part, stream)
+                             : a.type == kBf16 ? forward<bf16>(part, stream)
+                                               : forward<fp16>(part, stream);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_layer_norm_grad(const NormArgs& a, hipStream_t stream) {

@@ -1011,10 +1011,13 @@ __global__ __launch_bounds__(kProductThreads) void grad_weights(Product p, DwOut
     }
 }
 
-// No rows: the weights' gradient is zero.
-__global__ __launch_bounds__(256) void clear_weights(float* dw, int64_t stride, int64_t cols) {
+// No rows: the weights' gradient is zero.  64 rows of it a block.
+__global__ __launch_bounds__(256) void clear_weights(float* dw, int64_t stride, int64_t vocab,
+                                                     int64_t cols) {
     const int64_t c = int64_t(blockIdx.y) * 256 + threadIdx.x;
-    if (c < cols) dw[int64_t(blockIdx.x) * stride + c] = 0.0f;
+    if (c >= cols) return;
+    for (int64_t v = int64_t(blockIdx.x) * 64; v < std::min<int64_t>(vocab, int64_t(blockIdx.x) * 64 + 64); ++v)
+        dw[v * stride + c] = 0.0f;
 }
 
 // ------------------------------------------------------------- host: tiles
@@ -1128,6 +1131,10 @@ struct Arena {
 constexpr int64_t kPieceAlign = 256;
 constexpr int64_t kPad = 64;
 constexpr int64_t kMostBytes = int64_t(8) << 30;  // of a piece that `best` asks for
+// Largest piece: a tile's rows of P lie within 2^31 bytes (the buffer
+// descriptors' offsets), and the logits' tiles are at most 2^23 blocks (a
+// launch's threads are counted in 32 bits).
+constexpr int64_t kMostPiece = int64_t(1) << 21, kMostLogits = int64_t(1) << 39;
 
 struct Layout {
     // sizes
@@ -1210,8 +1217,9 @@ int64_t bytes_of(const VocabArgs& a, bool grad, int64_t piece) {
 // The largest piece that fits, the pieces then made equal.
 int64_t choose_piece(const VocabArgs& a, bool grad, int64_t bytes) {
     const int64_t all = up(a.vocab, kPieceAlign);
-    int64_t low = 1, high = all / kPieceAlign;  // in units of kPieceAlign
-    if (bytes_of(a, grad, all) <= bytes) return all;
+    const int64_t most = std::min({all, kMostPiece, kMostLogits / a.rows / kPieceAlign * kPieceAlign});
+    if (bytes_of(a, grad, most) <= bytes) return most;
+    int64_t low = 1, high = most / kPieceAlign;  // in units of kPieceAlign
     while (high - low > 1) {
         const int64_t mid = (low + high) / 2;
         (bytes_of(a, grad, mid * kPieceAlign) <= bytes ? low : high) = mid;
@@ -1452,8 +1460,9 @@ hipError_t launch_vocab_loss_grad(const VocabArgs& a, void* workspace, int64_t b
                                   hipStream_t stream) {
     if (a.rows == 0) {
         if (!a.dw || a.accumulate) return hipSuccess;
-        hipLaunchKernelGGL(clear_weights, dim3(unsigned(a.vocab), unsigned((a.cols + 255) / 256)),
-                           dim3(256), 0, stream, a.dw, a.dw_stride, a.cols);
+        hipLaunchKernelGGL(clear_weights,
+                           dim3(unsigned((a.vocab + 63) / 64), unsigned((a.cols + 255) / 256)), dim3(256),
+                           0, stream, a.dw, a.dw_stride, a.vocab, a.cols);
         return hipGetLastError();
     }
     Arena arena{static_cast<char*>(workspace)};

@@ -14,9 +14,10 @@
 namespace {
 
 constexpr int64_t kMaxNormRows = (int64_t(1) << 30) - 1, kMaxNormCols = int64_t(1) << 20;
-constexpr int64_t kMaxRows = int64_t(1) << 22, kMaxCols = int64_t(1) << 16;
-constexpr int64_t kMaxVocab = int64_t(1) << 24, kMaxStride = int64_t(1) << 22;
+constexpr int64_t kMaxRows = int64_t(1) << 21, kMaxCols = int64_t(1) << 16;
+constexpr int64_t kMaxVocab = int64_t(1) << 24, kMaxStride = int64_t(1) << 21;
 constexpr int kMaxTop = 1024;
+constexpr int64_t kMaxEntries = int64_t(1) << 30;
 constexpr uintptr_t kWorkspaceAlign = 256;
 
 // Sets the error message; without host memory for it the code alone is
@@ -115,10 +116,13 @@ int check_vocab(const phub::VocabArgs& a, bool grad) {
     return check_matrix("dw", a.dw, a.dw_stride, a.cols, kMaxStride, 4, false);
 }
 
-int check_teacher(int top, float temperature) {
+int check_teacher(int64_t rows, int top, float temperature) {
     if (int rc = check_size("top", top, 1, kMaxTop)) return rc;
-    if (!(temperature > 0.0f) || !std::isfinite(temperature) || !std::isfinite(1.0f / temperature))
-        return refuse("temperature %g is not a positive number", double(temperature));
+    if (int rc = check_size("rows", rows, 0, kMaxRows)) return rc;
+    if (rows * top > kMaxEntries)
+        return refuse("%lld rows of %d entries are more than 2^30", (long long)rows, top);
+    if (!(temperature >= 1e-6f && temperature <= 1e6f))
+        return refuse("temperature %g is outside [1e-6, 1e6]", double(temperature));
     return PHUB_OK;
 }
 
@@ -296,7 +300,7 @@ int phub_distill_loss(int type, int64_t rows, int64_t cols, int64_t vocab, const
                       int64_t x_stride, const void* w, int64_t w_stride, int top,
                       const int64_t* index, const float* logit, float temperature, float* loss_out,
                       float* lse, void* workspace, int64_t workspace_bytes, void* hip_stream) {
-    if (int rc = check_teacher(top, temperature)) return rc;
+    if (int rc = check_teacher(rows, top, temperature)) return rc;
     phub::VocabArgs a{};
     a.type = type;
     a.rows = rows;
@@ -321,7 +325,7 @@ int phub_distill_loss_grad(int type, int64_t rows, int64_t cols, int64_t vocab, 
                            const float* lse, const float* dloss, void* dx, int64_t dx_stride,
                            float* dw, int64_t dw_stride, int accumulate, void* workspace,
                            int64_t workspace_bytes, void* hip_stream) {
-    if (int rc = check_teacher(top, temperature)) return rc;
+    if (int rc = check_teacher(rows, top, temperature)) return rc;
     phub::VocabArgs a{};
     a.type = type;
     a.rows = rows;

@@ -164,6 +164,17 @@ def test_no_rows(torch):
     assert not dw.any() and not db.any()
 
 
+def test_more_rows_than_one_launch_takes(torch):
+    from paper_1805_07891_amd import layers
+    for cols in (24, 5):
+        x, dy, w, b = _inputs(torch, (1 << 20) + 77, cols, torch.bfloat16, seed=4)
+        y, mean, rstd = layers.layer_norm(x, w, b, EPS)
+        dw, db = torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+        dx = layers.layer_norm_grad(dy, x, w, mean, rstd, dw, db)
+        d = _definition(torch, x, dy, w, b)
+        _check(torch, x, dy, w, b, dict(y=y, mean=mean, rstd=rstd, dx=dx, dw=dw, db=db), d)
+
+
 def test_a_row_of_one_value_and_large_offsets(torch):
     from paper_1805_07891_amd import layers
     x = torch.full((4, 1000), 1e4, device="cuda")

@@ -69,10 +69,10 @@ LOSS = dict(type=0, rows=4, cols=8, vocab=10, x=P, xs=8, w=P, ws_=8, target=P, l
 
 
 @pytest.mark.parametrize("change, word", [
-    (dict(type=3), "type"), (dict(rows=-1), "rows"), (dict(rows=(1 << 22) + 1), "rows"),
+    (dict(type=3), "type"), (dict(rows=-1), "rows"), (dict(rows=(1 << 21) + 1), "rows"),
     (dict(cols=0), "cols"), (dict(cols=(1 << 16) + 1), "cols"), (dict(vocab=0), "vocab"),
     (dict(vocab=(1 << 24) + 1), "vocab"), (dict(x=None), "x is NULL"), (dict(x=P + 1), "x"),
-    (dict(xs=7), "x"), (dict(xs=(1 << 22) + 1), "x"), (dict(w=None), "w is NULL"),
+    (dict(xs=7), "x"), (dict(xs=(1 << 21) + 1), "x"), (dict(w=None), "w is NULL"),
     (dict(ws_=7), "w"), (dict(target=None), "target"), (dict(target=P + 4), "target"),
     (dict(loss=None), "loss"), (dict(lse=P + 2), "lse"), (dict(ws=None), "workspace"),
     (dict(ws=P + 128), "workspace"), (dict(n=1000), "needed")])
@@ -104,7 +104,8 @@ DISTILL_GRAD = dict(type=0, rows=4, cols=8, vocab=10, x=P, xs=8, w=P, ws_=8, top
     (dict(top=0), "top"), (dict(top=1025), "top"), (dict(index=None), "index"),
     (dict(logit=None), "logit"), (dict(logit=P + 2), "logit"), (dict(t=0.0), "temperature"),
     (dict(t=-1.0), "temperature"), (dict(t=float("nan")), "temperature"),
-    (dict(t=float("inf")), "temperature"), (dict(t=1e-45), "temperature"),
+    (dict(t=float("inf")), "temperature"), (dict(t=1e-7), "temperature"),
+    (dict(t=1e7), "temperature"), (dict(rows=(1 << 20) + 1, top=1024), "entries"),
     (dict(n=1000), "needed")])
 def test_distill_refuses(lib, change, word):
     _refused(lib, lib.phub_distill_loss, {**DISTILL, **change}.values(), word)
