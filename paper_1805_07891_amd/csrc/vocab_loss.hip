@@ -100,6 +100,7 @@ __global__ __launch_bounds__(256) void prepare_teacher(int64_t rows, int64_t voc
         if (mine >= 0) {
             bool again = false;
             q = 0.0f;
+#pragma unroll 8
             for (int m = 0; m < top; ++m) {
                 const bool same = idx[m] == mine;
                 if (same) q += val[m];
@@ -194,28 +195,39 @@ __device__ __forceinline__ int largest_of(const Largest& l) {
     return e == kNoExponent ? 0 : e;
 }
 
-// A block's word of the above: `e` is the wave's.
-__device__ __forceinline__ void leave_largest(int e, int* blocks) {
+// Word `block` of the above: `e` is the wave's.
+__device__ __forceinline__ void leave_largest(int e, int* blocks, int block) {
     __shared__ int words[4];
     if ((threadIdx.x & 63) == 0) words[threadIdx.x / 64] = e;
     __syncthreads();
     if (threadIdx.x == 0)
-        blocks[blockIdx.x] = max(max(words[0], words[1]), max(words[2], words[3]));
+        blocks[block] = max(max(words[0], words[1]), max(words[2], words[3]));
 }
 
 // Rows as the product takes them, `ld` elements apart, zero from cols on:
 // fp32 as two fp16 planes, with each row's exponent and the power of two that
 // undoes its scale; 16-bit types as they are.  A wave a row at a time.
+struct PackArgs {
+    int blocks;  // 0: nothing to pack
+    const void* src;
+    int64_t stride, rows;
+    void* dst;
+    int64_t plane;
+    float* scale;       // these three of fp32 types
+    int* row_exponent;  // may be null
+    int* largest;       // may be null
+};
+
 template <typename T>
-__global__ __launch_bounds__(256) void pack_rows(const T* src, int64_t stride, int64_t rows, int cols,
-                                                 void* dst, int64_t ld, int64_t plane, float* scale,
-                                                 int* row_exponent, int* largest) {
+__device__ __forceinline__ void pack_rows(const PackArgs& a, int block, int cols, int64_t ld) {
     constexpr int E = kPerLoad<T>;
     const int lane = int(threadIdx.x) & 63;
+    const int64_t plane = a.plane;
+    void* const dst = a.dst;
     int most = kNoExponent;
-    for (int64_t row = int64_t(blockIdx.x) * 4 + threadIdx.x / 64; row < rows;
-         row += int64_t(gridDim.x) * 4) {
-        const T* const p = src + row * stride;
+    for (int64_t row = int64_t(block) * 4 + threadIdx.x / 64; row < a.rows;
+         row += int64_t(a.blocks) * 4) {
+        const T* const p = static_cast<const T*>(a.src) + row * a.stride;
         const int whole = cols / E;
         int e = 0;
         if constexpr (std::is_same<T, float>::value) {
@@ -223,8 +235,8 @@ __global__ __launch_bounds__(256) void pack_rows(const T* src, int64_t stride, i
             e = exponent_of(row_largest<T>(p, cols, r));
             most = max(most, e);
             if (lane == 0) {
-                scale[row] = __builtin_amdgcn_ldexpf(1.0f, e - 14);
-                if (row_exponent) row_exponent[row] = e;
+                a.scale[row] = __builtin_amdgcn_ldexpf(1.0f, e - 14);
+                if (a.row_exponent) a.row_exponent[row] = e;
             }
             for (int first = 0; first < whole; first += 64 * kBatch) {
                 // (a row of one batch is in registers already)
@@ -269,59 +281,89 @@ __global__ __launch_bounds__(256) void pack_rows(const T* src, int64_t stride, i
             }
         }
     }
-    if (largest) leave_largest(most, largest);
+    if (a.largest) leave_largest(most, a.largest, block);
 }
 
 // What the backward pass needs of each row: whether it has a target (alive: all bits
 // or none), its factor g T, the exponent of x and the block's largest of factor x.  A
 // wave a row at a time.
+struct RowsArgs {
+    int blocks;  // 0: a forward pass
+    const void* x;
+    int64_t stride, rows;
+    const int* teacher_alive;
+    const float* dloss;
+    float temperature;
+    int* alive;
+    float* factor;
+    int* row_exponent;
+    int* largest;
+};
+
 template <typename T>
-__global__ __launch_bounds__(256) void prepare_rows(const T* x, int64_t x_stride, int64_t rows,
-                                                    int cols, Targets t, const int* teacher_alive,
-                                                    const float* dloss, float temperature,
-                                                    int* alive, float* factor, int* row_exponent,
-                                                    int* largest) {
+__device__ __forceinline__ void describe_rows(const RowsArgs& a, const Targets& t, int block, int cols) {
     const int lane = int(threadIdx.x) & 63;
     int most = kNoExponent;
-    for (int64_t row = int64_t(blockIdx.x) * 4 + threadIdx.x / 64; row < rows;
-         row += int64_t(gridDim.x) * 4) {
-        const T* const xr = x + row * x_stride;
-        const bool live = teacher_alive ? teacher_alive[row] != 0 : index_of(t, row, 0) >= 0;
-        const float f = !live ? 0.0f : (dloss ? dloss[row] : 1.0f) * temperature;
+    for (int64_t row = int64_t(block) * 4 + threadIdx.x / 64; row < a.rows;
+         row += int64_t(a.blocks) * 4) {
+        const bool live = a.teacher_alive ? a.teacher_alive[row] != 0 : index_of(t, row, 0) >= 0;
+        const float f = !live ? 0.0f : (a.dloss ? a.dloss[row] : 1.0f) * a.temperature;
         Piece<T> r[kBatch];
-        const int e = exponent_of(row_largest<T>(xr, cols, r));
+        const int e =
+            exponent_of(row_largest<T>(static_cast<const T*>(a.x) + row * a.stride, cols, r));
         if (lane == 0) {
-            alive[row] = live ? -1 : 0;
-            factor[row] = f;
-            row_exponent[row] = e;
+            a.alive[row] = live ? -1 : 0;
+            a.factor[row] = f;
+            a.row_exponent[row] = e;
         }
         const float size = __builtin_fabsf(f);
         if (size > 0.0f && size < __builtin_huge_valf())
             most = max(most, e + __builtin_amdgcn_frexp_expf(size));
     }
-    leave_largest(most, largest);
+    leave_largest(most, a.largest, block);
+}
+
+// The three in one launch, a run of blocks each.
+template <typename T>
+__global__ __launch_bounds__(256) void prepare(PackArgs x, PackArgs w, RowsArgs rows, Targets t,
+                                               int cols, int64_t ld) {
+    int block = int(blockIdx.x);
+    if (block < x.blocks) return pack_rows<T>(x, block, cols, ld);
+    block -= x.blocks;
+    if (block < w.blocks) return pack_rows<T>(w, block, cols, ld);
+    describe_rows<T>(rows, t, block - w.blocks, cols);
 }
 
 // dst[c][r] = src[r][c] for columns c < cols, and zero for rows up to ld (a
 // multiple of 64) that do not exist or are not alive: a column tile of 64
 // and 64 rows a block.  SCALED: as fp16 (planes), scaled by the row's exponent;
 // otherwise as it is.
-template <typename T, bool SCALED>
-__global__ __launch_bounds__(256) void transpose(const T* src, int64_t stride, int64_t rows, int cols,
-                                                 void* dst, int64_t ld, int64_t plane, int planes,
-                                                 const int* row_exponent, const int* alive) {
-    __shared__ float tile[64][65];
+struct TransposeArgs {
+    int tiles;  // of rows; 0: nothing to transpose
+    const void* src;
+    int64_t stride, rows;
+    void* dst;
+    int64_t ld, plane;
+    const int* row_exponent;
+    const int* alive;  // may be null
+};
+
+template <typename T, bool SCALED, int PLANES>
+__device__ __forceinline__ void transpose(const TransposeArgs& a, int block_r, int block_c, int cols,
+                                          float (&tile)[64][65]) {
     constexpr int E = kPerLoad<T>;
-    const int64_t r0 = int64_t(blockIdx.x) * 64;
-    const int c0 = int(blockIdx.y) * 64;
+    const T* const src = static_cast<const T*>(a.src);
+    const int64_t stride = a.stride, rows = a.rows, ld = a.ld;
+    const int64_t r0 = int64_t(block_r) * 64;
+    const int c0 = block_c * 64;
     constexpr int PER_ROW = 64 / E;  // pieces of a row of the tile
     for (int u = int(threadIdx.x); u < 64 * PER_ROW; u += 256) {
         const int r = u / PER_ROW, c = u % PER_ROW * E;
         const int64_t row = r0 + r;
-        const bool in = row < rows && (!alive || alive[row]);
+        const bool in = row < rows && (!a.alive || a.alive[row]);
         Piece<T> p = {};
         if (in && c0 + c < cols) p = load_piece<T>(src + row * stride + c0 + c, cols - c0 - c);
-        const int e = SCALED && in ? row_exponent[row] : 0;
+        const int e = SCALED && in ? a.row_exponent[row] : 0;
 #pragma unroll
         for (int i = 0; i < E; ++i)
             tile[r][c + i] = SCALED ? __builtin_amdgcn_ldexpf(float(p.e[i]), 14 - e) : float(p.e[i]);
@@ -329,7 +371,7 @@ __global__ __launch_bounds__(256) void transpose(const T* src, int64_t stride, i
     __syncthreads();
     typedef typename std::conditional<SCALED, fp16, T>::type O;
     if constexpr (sizeof(O) == 2) {
-        O* const out = static_cast<O*>(dst);
+        O* const out = static_cast<O*>(a.dst);
         for (int u = int(threadIdx.x); u < 64 * 8; u += 256) {
             const int c = u / 8, r = u % 8 * 8;
             if (c0 + c >= cols) continue;
@@ -342,9 +384,20 @@ __global__ __launch_bounds__(256) void transpose(const T* src, int64_t stride, i
             }
             O* const at = out + int64_t(c0 + c) * ld + r0 + r;
             __builtin_memcpy(at, h, 16);
-            if (planes == 2) __builtin_memcpy(at + plane, l, 16);
+            if constexpr (PLANES == 2) __builtin_memcpy(at + a.plane, l, 16);
         }
     }
+}
+
+// x for the product of dw and w for that of dx, in one launch.
+template <typename T, int PLANES>
+__global__ __launch_bounds__(256) void transposes(TransposeArgs x, TransposeArgs w, int cols) {
+    __shared__ float tile[64][65];
+    const int block = int(blockIdx.x);
+    if (block < x.tiles)
+        transpose<T, true, PLANES>(x, block, int(blockIdx.y), cols, tile);
+    else
+        transpose<T, PLANES == 2, PLANES>(w, block - x.tiles, int(blockIdx.y), cols, tile);
 }
 
 // ------------------------------------------------------- the product's users
@@ -1248,22 +1301,25 @@ int row_blocks(int64_t rows) {
     return int(std::min<int64_t>((rows + 3) / 4, kExponentBlocks));
 }
 
-template <typename S>
-hipError_t pack(const S* src, int64_t stride, int64_t rows, const VocabArgs& a, const Layout& l,
-                char* dst, int64_t plane_rows, float* scale, int* row_exponent, int* largest,
-                hipStream_t stream) {
-    hipLaunchKernelGGL(pack_rows<S>, dim3(unsigned(row_blocks(rows))), dim3(256), 0, stream, src,
-                       stride, rows, int(a.cols), static_cast<void*>(dst), l.packed_ld,
-                       plane_rows * l.packed_ld, scale, row_exponent, largest);
-    return hipGetLastError();
+// How x is packed, or a piece of w: not at all if the product can read it.
+PackArgs pack_x(const VocabArgs& a, const Layout& l) {
+    return {l.pack_x ? row_blocks(a.rows) : 0, a.x, a.x_stride, a.rows, l.x, a.rows * l.packed_ld,
+            l.scale_x, nullptr, nullptr};
 }
 
-// The rows of x as the logits' product takes them.
+PackArgs pack_w(const VocabArgs& a, const Layout& l, const void* w, int64_t rows) {
+    return {l.pack_w ? row_blocks(rows) : 0, w, a.w_stride, rows, l.w, l.piece * l.packed_ld,
+            l.scale_w, l.w_exponent, l.largest_w};
+}
+
 template <typename S>
-hipError_t pack_x(const VocabArgs& a, const Layout& l, hipStream_t stream) {
-    if (!l.pack_x) return hipSuccess;
-    return pack(static_cast<const S*>(a.x), a.x_stride, a.rows, a, l, l.x, a.rows, l.scale_x,
-                static_cast<int*>(nullptr), static_cast<int*>(nullptr), stream);
+hipError_t launch_prepare(const VocabArgs& a, const Layout& l, const PackArgs& x, const PackArgs& w,
+                          const RowsArgs& rows, hipStream_t stream) {
+    const int blocks = x.blocks + w.blocks + rows.blocks;
+    if (blocks == 0) return hipSuccess;
+    hipLaunchKernelGGL(prepare<S>, dim3(unsigned(blocks)), dim3(256), 0, stream, x, w, rows,
+                       targets_of(a, l), int(a.cols), l.packed_ld);
+    return hipGetLastError();
 }
 
 template <typename O>
@@ -1276,27 +1332,22 @@ hipError_t join(const float* part, int splits, int64_t rows, const VocabArgs& a,
 
 struct PieceAt {
     int64_t first, rows;
+    const void* w;
 };
 
 PieceAt piece_at(const VocabArgs& a, const Layout& l, int64_t i) {
-    return {i * l.piece, std::min(l.piece, a.vocab - i * l.piece)};
+    const int64_t first = i * l.piece, size = a.type == kF32 ? 4 : 2;
+    return {first, std::min(l.piece, a.vocab - first),
+            static_cast<const char*>(a.w) + first * a.w_stride * size};
 }
 
-// The operands of a piece's logits, w's rows packed first where they have to
-// be.
-template <typename S>
-hipError_t logits_of(const VocabArgs& a, const Layout& l, int64_t i, Operand* x, Operand* w,
-                     Product* p, Logits* z, hipStream_t stream) {
-    const PieceAt at = piece_at(a, l, i);
-    const S* const from = static_cast<const S*>(a.w) + at.first * a.w_stride;
-    if (l.pack_w) {
-        hipError_t e = pack(from, a.w_stride, at.rows, a, l, l.w, l.piece, l.scale_w, l.w_exponent,
-                            l.largest_w, stream);
-        if (e != hipSuccess) return e;
+// The operands of a piece's logits.
+void logits_of(const VocabArgs& a, const Layout& l, const PieceAt& at, Operand* x, Operand* w,
+               Product* p, Logits* z) {
+    if (l.pack_w)
         *w = {l.w, l.packed_ld, l.piece * l.packed_ld, int(at.rows)};
-    } else {
-        *w = {from, a.w_stride, 0, int(at.rows)};
-    }
+    else
+        *w = {at.w, a.w_stride, 0, int(at.rows)};
     if (l.pack_x)
         *x = {l.x, l.packed_ld, a.rows * l.packed_ld, int(a.rows)};
     else
@@ -1305,7 +1356,6 @@ hipError_t logits_of(const VocabArgs& a, const Layout& l, int64_t i, Operand* x,
     p->segments = l.planes == 2 ? 3 : 1;
     *z = {int(a.rows), int(at.rows), 1.0f / a.temperature, l.scale_x, l.scale_w,
           a.top ? nullptr : a.target, at.first};
-    return hipSuccess;
 }
 
 // The logits of a teacher's entries in a piece.  Few pairs are spread over more
@@ -1328,13 +1378,15 @@ hipError_t pick_of(const VocabArgs& a, const Layout& l, const Operand& x, const 
 template <typename S, typename T>
 hipError_t loss_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
     hipError_t e = teacher_of(a, l, stream);
-    if (e == hipSuccess) e = pack_x<S>(a, l, stream);
     int blocks = 0;
     for (int64_t i = 0; i < l.pieces && e == hipSuccess; ++i) {
+        const PieceAt at = piece_at(a, l, i);
+        e = launch_prepare<S>(a, l, i == 0 ? pack_x(a, l) : PackArgs{}, pack_w(a, l, at.w, at.rows),
+                              RowsArgs{}, stream);
+        if (e != hipSuccess) break;
         Product p;
         Logits z;
-        e = logits_of<S>(a, l, i, &p.c, &p.r, &p, &z, stream);
-        if (e != hipSuccess) break;
+        logits_of(a, l, at, &p.c, &p.r, &p, &z);
         const ForwardOut o{l.part, blocks, l.pick};
         if constexpr (std::is_same<S, float>::value)
             e = run_forward<T, kScaledRows>(l.shape, p, z, o, stream);
@@ -1358,26 +1410,33 @@ hipError_t grad_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
     const Targets targets = targets_of(a, l);
     const Largest largest{l.largest, row_blocks(a.rows)};
     hipError_t e = teacher_of(a, l, stream);
-    if (e == hipSuccess) e = pack_x<S>(a, l, stream);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(prepare_rows<S>, dim3(unsigned(row_blocks(a.rows))), dim3(256), 0, stream,
-                       static_cast<const S*>(a.x), a.x_stride, a.rows, int(a.cols), targets,
-                       l.teacher_alive, a.dloss, a.temperature, l.alive, l.factor, l.row_exponent,
-                       l.largest);
-    if (a.dw) {
-        const dim3 by_tile(unsigned(up(a.rows, 64) / 64), unsigned((a.cols + 63) / 64));
-        hipLaunchKernelGGL((transpose<S, true>), by_tile, dim3(256), 0, stream,
-                           static_cast<const S*>(a.x), a.x_stride, a.rows, int(a.cols),
-                           static_cast<void*>(l.xt), l.rows_ld, a.cols * l.rows_ld, PLANES,
-                           l.row_exponent, l.alive);
-    }
-    if ((e = hipGetLastError()) != hipSuccess) return e;
     for (int64_t i = 0; i < l.pieces; ++i) {
         const PieceAt at = piece_at(a, l, i);
         const Largest largest_w{l.largest_w, row_blocks(at.rows)};
+        RowsArgs rows{};
+        if (i == 0)
+            rows = {row_blocks(a.rows), a.x, a.x_stride, a.rows, l.teacher_alive, a.dloss, a.temperature,
+                    l.alive, l.factor, l.row_exponent, l.largest};
+        e = launch_prepare<S>(a, l, i == 0 ? pack_x(a, l) : PackArgs{}, pack_w(a, l, at.w, at.rows), rows,
+                              stream);
+        if (e != hipSuccess) return e;
+        TransposeArgs tx{}, tw{};
+        if (a.dw && i == 0)
+            tx = {int(up(a.rows, 64) / 64), a.x, a.x_stride, a.rows, l.xt, l.rows_ld, a.cols * l.rows_ld,
+                  l.row_exponent, l.alive};
+        if (a.dx)
+            tw = {int(up(at.rows, 64) / 64), at.w, a.w_stride, at.rows, l.wt, l.ld_p, a.cols * l.ld_p,
+                  l.w_exponent, nullptr};
+        if (tx.tiles + tw.tiles > 0) {
+            hipLaunchKernelGGL((transposes<S, PLANES>),
+                               dim3(unsigned(tx.tiles + tw.tiles), unsigned((a.cols + 63) / 64)),
+                               dim3(256), 0, stream, tx, tw, int(a.cols));
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+        }
         Product p;
         Logits z;
-        if ((e = logits_of<S>(a, l, i, &p.r, &p.c, &p, &z, stream)) != hipSuccess) return e;
+        logits_of(a, l, at, &p.r, &p.c, &p, &z);
         const BackwardOut o{a.lse, l.alive, l.factor, l.row_exponent, largest, largest_w,
                             l.p, l.ld_p, a.rows * l.ld_p, l.q, l.rows_ld, l.piece * l.rows_ld};
         e = !a.dw   ? run_backward<T, PLANES, 1>(l.shape, p, z, o, stream)
@@ -1393,17 +1452,10 @@ hipError_t grad_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
         if (a.dx) {
-            const int64_t k = up(at.rows, 64);
-            const S* const w = static_cast<const S*>(a.w) + at.first * a.w_stride;
-            const dim3 by_tile(unsigned(k / 64), unsigned((a.cols + 63) / 64));
-            hipLaunchKernelGGL((transpose<S, PLANES == 2>), by_tile, dim3(256), 0, stream, w,
-                               a.w_stride, at.rows, int(a.cols), static_cast<void*>(l.wt), l.ld_p,
-                               a.cols * l.ld_p, PLANES, l.w_exponent, nullptr);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
             Product d;
             d.r = {l.wt, l.ld_p, a.cols * l.ld_p, int(a.cols)};
             d.c = {l.p, l.ld_p, a.rows * l.ld_p, int(a.rows)};
-            d.k = int(k);
+            d.k = int(up(at.rows, 64));
             d.segments = PLANES == 2 ? 3 : 1;
             d.splits = l.dx_plan.splits;
             DxOut x{l.alive, l.factor, largest_w, l.part_x ? nullptr : a.dx, a.dx_stride, l.part_x,
