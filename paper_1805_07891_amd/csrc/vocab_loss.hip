@@ -60,23 +60,37 @@ __device__ __forceinline__ int index_of(const Targets& t, int64_t row, int k) {
     return v >= 0 && v < t.vocab ? int(v) : -1;
 }
 
-// A wave a row.  entropy: sum of q log q.
-__global__ __launch_bounds__(256) void prepare_teacher(int64_t rows, int64_t vocab, int top,
-                                                       const int64_t* target, const float* logit,
-                                                       float temperature, int* index,
-                                                       float* weight, int* alive, float* entropy) {
-    extern __shared__ float words[];  // top floats and top ints a wave
-    const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) / 64;
-    const int64_t i = int64_t(blockIdx.x) * 4 + wave;
-    if (i >= rows) return;
+// A teacher's distribution, a wave a row.  entropy: sum of q log q.
+struct TeacherArgs {
+    int blocks;  // 0: targets
+    int64_t rows, vocab;
+    int top;
+    const int64_t* entry;
+    const float* logit;
+    float temperature;
+    int* index;
+    float* weight;
+    int* alive;
+    float* entropy;
+};
+
+__device__ __forceinline__ bool is_entry(int64_t v, int64_t vocab, float logit) {
+    return v >= 0 && v < vocab && logit != -__builtin_huge_valf();
+}
+
+// words: top floats and top ints a wave
+__device__ __forceinline__ void prepare_teacher(const TeacherArgs& a, int block, float* words) {
+    const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) / 64, top = a.top;
+    const int64_t i = int64_t(block) * 4 + wave;
+    if (i >= a.rows) return;
     float* const val = words + 2 * top * wave;
     int* const idx = reinterpret_cast<int*>(val + top);
-    const float inv = 1.0f / temperature, low = -__builtin_huge_valf();
+    const float inv = 1.0f / a.temperature, low = -__builtin_huge_valf();
     float most = low;
     for (int k = lane; k < top; k += 64) {
-        const int64_t t = target[i * top + k];
-        const float l = logit[i * top + k];
-        const bool in = t >= 0 && t < vocab && l != low;
+        const int64_t t = a.entry[i * top + k];
+        const float l = a.logit[i * top + k];
+        const bool in = is_entry(t, a.vocab, l);
         idx[k] = in ? int(t) : -1;
         val[k] = in ? l * inv : low;
         if (in) most = l * inv > most || l != l ? l * inv : most;
@@ -110,13 +124,13 @@ __global__ __launch_bounds__(256) void prepare_teacher(int64_t rows, int64_t voc
         }
         if (mine < 0) q = 0.0f;
         if (q != 0.0f) ent += q * logf(q);
-        index[i * top + k] = mine;
-        weight[i * top + k] = q;
+        a.index[i * top + k] = mine;
+        a.weight[i * top + k] = q;
     }
     ent = wave_sum(ent);
     if (lane == 0) {
-        alive[i] = live;
-        if (entropy) entropy[i] = ent;
+        a.alive[i] = live;
+        a.entropy[i] = ent;
     }
 }
 
@@ -291,7 +305,6 @@ struct RowsArgs {
     int blocks;  // 0: a forward pass
     const void* x;
     int64_t stride, rows;
-    const int* teacher_alive;
     const float* dloss;
     float temperature;
     int* alive;
@@ -301,12 +314,18 @@ struct RowsArgs {
 };
 
 template <typename T>
-__device__ __forceinline__ void describe_rows(const RowsArgs& a, const Targets& t, int block, int cols) {
+__device__ __forceinline__ void describe_rows(const RowsArgs& a, const Targets& t,
+                                              const TeacherArgs& teacher, int block, int cols) {
     const int lane = int(threadIdx.x) & 63;
     int most = kNoExponent;
     for (int64_t row = int64_t(block) * 4 + threadIdx.x / 64; row < a.rows;
          row += int64_t(a.blocks) * 4) {
-        const bool live = a.teacher_alive ? a.teacher_alive[row] != 0 : index_of(t, row, 0) >= 0;
+        bool live = t.target && index_of(t, row, 0) >= 0;
+        if (!t.target)
+            for (int k = lane; k < teacher.top; k += 64)
+                live |= is_entry(teacher.entry[row * teacher.top + k], teacher.vocab,
+                                 teacher.logit[row * teacher.top + k]);
+        live = __any(live);
         const float f = !live ? 0.0f : (a.dloss ? a.dloss[row] : 1.0f) * a.temperature;
         Piece<T> r[kBatch];
         const int e =
@@ -323,15 +342,19 @@ __device__ __forceinline__ void describe_rows(const RowsArgs& a, const Targets& 
     leave_largest(most, a.largest, block);
 }
 
-// The three in one launch, a run of blocks each.
+// All of these in one launch, a run of blocks each: the teacher's first, which
+// take longest.
 template <typename T>
-__global__ __launch_bounds__(256) void prepare(PackArgs x, PackArgs w, RowsArgs rows, Targets t,
-                                               int cols, int64_t ld) {
+__global__ __launch_bounds__(256) void prepare(TeacherArgs teacher, PackArgs x, PackArgs w,
+                                               RowsArgs rows, Targets t, int cols, int64_t ld) {
+    extern __shared__ float words[];
     int block = int(blockIdx.x);
+    if (block < teacher.blocks) return prepare_teacher(teacher, block, words);
+    block -= teacher.blocks;
     if (block < x.blocks) return pack_rows<T>(x, block, cols, ld);
     block -= x.blocks;
     if (block < w.blocks) return pack_rows<T>(w, block, cols, ld);
-    describe_rows<T>(rows, t, block - w.blocks, cols);
+    describe_rows<T>(rows, t, teacher, block - w.blocks, cols);
 }
 
 // dst[c][r] = src[r][c] for columns c < cols, and zero for rows up to ld (a
@@ -529,12 +552,11 @@ __global__ __launch_bounds__(kProductThreads) void logits_forward(Product p, Log
 // error of the entry's logit that lse does not share stays whole in
 // softmax - q (with dot products of their own, fp32 gradients were 4e-6 off
 // instead of 1e-6).  Fragments come straight from memory, as no two pairs share
-// rows of w, those of the next kAhead instructions while this many are done.
-template <typename T, int PAIRS>
+// rows of w, those of the next AHEAD instructions while this many are done.
+template <typename T, int PAIRS, int AHEAD>
 __global__ __launch_bounds__(256) void target_logits(Operand x, Operand w, int k, int segments,
                                                      Targets t, Logits l, float* pick) {
     typedef typename Frag<T>::type F;
-    constexpr int kAhead = 8;
     const int lane = int(threadIdx.x) & 63, n = lane & 31, half = lane >> 5;
     const int64_t pair = (int64_t(blockIdx.x) * 4 + threadIdx.x / 64) * PAIRS + n;
     const int64_t row = pair / t.top;
@@ -545,7 +567,7 @@ __global__ __launch_bounds__(256) void target_logits(Operand x, Operand w, int k
     const T* const xr = static_cast<const T*>(x.base) + (in ? row : 0) * x.ld + half * 8;
     const T* const wr = static_cast<const T*>(w.base) + (in ? v : 0) * w.ld + half * 8;
     struct Ahead {
-        F x[kAhead], w[kAhead];
+        F x[AHEAD], w[AHEAD];
     };
     // one past the end of the segments' loops is loaded as zeros
     int seg = 0, at = 0;
@@ -553,14 +575,14 @@ __global__ __launch_bounds__(256) void target_logits(Operand x, Operand w, int k
         const T* const xs = xr + (seg == 1 ? x.plane : 0) + at;  // planes as of (R, C) = (w, x)
         const T* const ws = wr + (seg == 2 ? w.plane : 0) + at;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
+        for (int u = 0; u < AHEAD; ++u) {
             f.x[u] = f.w[u] = F{};
             if (in && seg < segments && at + u * 16 + half * 8 < k) {
                 f.x[u] = *reinterpret_cast<const F*>(xs + u * 16);
                 f.w[u] = *reinterpret_cast<const F*>(ws + u * 16);
             }
         }
-        at += 16 * kAhead;
+        at += 16 * AHEAD;
         if (at >= k) {
             at = 0;
             ++seg;
@@ -569,7 +591,7 @@ __global__ __launch_bounds__(256) void target_logits(Operand x, Operand w, int k
     f32x16 acc{};
     auto add = [&](const Ahead& f) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) acc = mfma(f.w[u], f.x[u], acc);
+        for (int u = 0; u < AHEAD; ++u) acc = mfma(f.w[u], f.x[u], acc);
     };
     Ahead f0, f1;
     fetch(f0);
@@ -1288,14 +1310,6 @@ Targets targets_of(const VocabArgs& a, const Layout& l) {
     return {std::max(1, a.top), int(a.vocab), a.top ? nullptr : a.target, l.index, l.weight};
 }
 
-hipError_t teacher_of(const VocabArgs& a, const Layout& l, hipStream_t stream) {
-    if (a.top == 0) return hipSuccess;
-    hipLaunchKernelGGL(prepare_teacher, dim3(unsigned((a.rows + 3) / 4)), dim3(256),
-                       unsigned(a.top) * 32, stream, a.rows, a.vocab, a.top, a.target, a.logit,
-                       a.temperature, l.index, l.weight, l.teacher_alive, l.entropy);
-    return hipGetLastError();
-}
-
 // Blocks of four waves that take `rows` rows in turn.
 int row_blocks(int64_t rows) {
     return int(std::min<int64_t>((rows + 3) / 4, kExponentBlocks));
@@ -1313,11 +1327,17 @@ PackArgs pack_w(const VocabArgs& a, const Layout& l, const void* w, int64_t rows
 }
 
 template <typename S>
-hipError_t launch_prepare(const VocabArgs& a, const Layout& l, const PackArgs& x, const PackArgs& w,
-                          const RowsArgs& rows, hipStream_t stream) {
-    const int blocks = x.blocks + w.blocks + rows.blocks;
+hipError_t launch_prepare(const VocabArgs& a, const Layout& l, bool is_first, const PackArgs& x,
+                          const PackArgs& w, const RowsArgs& rows, hipStream_t stream) {
+    // (rows, entries and what else a pass prepares once come with its first piece)
+    TeacherArgs teacher{};
+    if (a.top)
+        teacher = {is_first ? int((a.rows + 3) / 4) : 0, a.rows, a.vocab, a.top, a.target, a.logit,
+                   a.temperature, l.index, l.weight, l.teacher_alive, l.entropy};
+    const int blocks = teacher.blocks + x.blocks + w.blocks + rows.blocks;
     if (blocks == 0) return hipSuccess;
-    hipLaunchKernelGGL(prepare<S>, dim3(unsigned(blocks)), dim3(256), 0, stream, x, w, rows,
+    hipLaunchKernelGGL(prepare<S>, dim3(unsigned(blocks)), dim3(256),
+                       teacher.blocks ? unsigned(a.top) * 32 : 0, stream, teacher, x, w, rows,
                        targets_of(a, l), int(a.cols), l.packed_ld);
     return hipGetLastError();
 }
@@ -1366,10 +1386,10 @@ hipError_t pick_of(const VocabArgs& a, const Layout& l, const Operand& x, const 
     if (a.top == 0) return hipSuccess;
     const int64_t pairs = a.rows * a.top;
     if (pairs < 4 * kUnits * 32)
-        hipLaunchKernelGGL((target_logits<T, 8>), dim3(unsigned((pairs + 31) / 32)), dim3(256), 0,
+        hipLaunchKernelGGL((target_logits<T, 8, 16>), dim3(unsigned((pairs + 31) / 32)), dim3(256), 0,
                            stream, x, w, p.k, p.segments, targets_of(a, l), z, l.pick);
     else
-        hipLaunchKernelGGL((target_logits<T, 32>), dim3(unsigned((pairs + 127) / 128)), dim3(256), 0,
+        hipLaunchKernelGGL((target_logits<T, 32, 8>), dim3(unsigned((pairs + 127) / 128)), dim3(256), 0,
                            stream, x, w, p.k, p.segments, targets_of(a, l), z, l.pick);
     return hipGetLastError();
 }
@@ -1377,12 +1397,12 @@ hipError_t pick_of(const VocabArgs& a, const Layout& l, const Operand& x, const 
 // S: element type of x and w; T: of the products of logits and dx.
 template <typename S, typename T>
 hipError_t loss_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
-    hipError_t e = teacher_of(a, l, stream);
+    hipError_t e = hipSuccess;
     int blocks = 0;
     for (int64_t i = 0; i < l.pieces && e == hipSuccess; ++i) {
         const PieceAt at = piece_at(a, l, i);
-        e = launch_prepare<S>(a, l, i == 0 ? pack_x(a, l) : PackArgs{}, pack_w(a, l, at.w, at.rows),
-                              RowsArgs{}, stream);
+        e = launch_prepare<S>(a, l, i == 0, i == 0 ? pack_x(a, l) : PackArgs{},
+                              pack_w(a, l, at.w, at.rows), RowsArgs{}, stream);
         if (e != hipSuccess) break;
         Product p;
         Logits z;
@@ -1409,17 +1429,16 @@ hipError_t grad_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
     constexpr int PLANES = std::is_same<S, float>::value ? 2 : 1;
     const Targets targets = targets_of(a, l);
     const Largest largest{l.largest, row_blocks(a.rows)};
-    hipError_t e = teacher_of(a, l, stream);
-    if (e != hipSuccess) return e;
+    hipError_t e = hipSuccess;
     for (int64_t i = 0; i < l.pieces; ++i) {
         const PieceAt at = piece_at(a, l, i);
         const Largest largest_w{l.largest_w, row_blocks(at.rows)};
         RowsArgs rows{};
         if (i == 0)
-            rows = {row_blocks(a.rows), a.x, a.x_stride, a.rows, l.teacher_alive, a.dloss, a.temperature,
-                    l.alive, l.factor, l.row_exponent, l.largest};
-        e = launch_prepare<S>(a, l, i == 0 ? pack_x(a, l) : PackArgs{}, pack_w(a, l, at.w, at.rows), rows,
-                              stream);
+            rows = {row_blocks(a.rows), a.x, a.x_stride, a.rows, a.dloss, a.temperature, l.alive,
+                    l.factor, l.row_exponent, l.largest};
+        e = launch_prepare<S>(a, l, i == 0, i == 0 ? pack_x(a, l) : PackArgs{},
+                              pack_w(a, l, at.w, at.rows), rows, stream);
         if (e != hipSuccess) return e;
         TransposeArgs tx{}, tw{};
         if (a.dw && i == 0)
