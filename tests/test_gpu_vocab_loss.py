@@ -259,6 +259,74 @@ def test_accumulate_either_gradient_alone_and_repeats(torch):
     assert torch.equal(loss, l2)
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
+@pytest.mark.parametrize("rows, cols, vocab, top", [(5, 40, 300, 0), (1100, 96, 4100, 0),
+                                                    (2100, 72, 8200, 0), (1100, 64, 4100, 33)])
+def test_either_gradient_alone_has_the_same_bits(torch, rows, cols, vocab, top, dtype):
+    from paper_1805_07891_amd import layers
+    dtype = getattr(torch, dtype)
+    x, w, *target, dloss = _inputs(torch, rows, cols, vocab, dtype, top)
+    loss = layers.distill_loss if top else layers.vocab_loss
+    grad = layers.distill_loss_grad if top else layers.vocab_loss_grad
+    args = (*target, 2.0) if top else target
+    _, lse = loss(x, w, *args)
+    dw, alone = torch.empty(vocab, cols, device="cuda"), torch.empty(vocab, cols, device="cuda")
+    dx = grad(x, w, *args, lse, dloss, dw)
+    assert grad(x, w, *args, lse, dloss, alone, want_dx=False) is None
+    assert torch.equal(alone, dw)
+    assert torch.equal(grad(x, w, *args, lse, dloss), dx)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_pieces_of_the_vocabulary_with_a_teacher(torch, dtype):
+    from paper_1805_07891_amd import layers
+    dtype = getattr(torch, dtype)
+    rows, cols, vocab, top, t = 130, 72, 1500, 21, 1.5
+    x, w, index, logits, dloss = _inputs(torch, rows, cols, vocab, dtype, top)
+    d = _definition(torch, x, w, index, logits, t, dloss)
+    for most in (0, 1 << 20, None):
+        space = layers.vocab_workspace(x, w, top, most=most)
+        loss, lse = layers.distill_loss(x, w, index, logits, t, workspace=space)
+        _check_loss(d, loss, lse)
+        dw = torch.full((vocab, cols), 7.0, device="cuda")
+        dx = layers.distill_loss_grad(x, w, index, logits, t, lse, dloss, dw, workspace=space)
+        _check_grad(torch, d, dx, dw, dtype, pieces=8)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_many_rows_few_entries_and_accumulation(torch, dtype):
+    """The weights' gradient in parts over the rows, added to what is there."""
+    from paper_1805_07891_amd import layers
+    dtype = getattr(torch, dtype)
+    x, w, target, dloss = _inputs(torch, 5000, 64, 100, dtype)
+    d = _definition(torch, x, w, target, None, 1.0, dloss)
+    loss, lse = layers.vocab_loss(x, w, target)
+    _check_loss(d, loss, lse)
+    dw = torch.full((100, 64), 7.0, device="cuda")
+    dx = layers.vocab_loss_grad(x, w, target, lse, dloss, dw)
+    _check_grad(torch, d, dx, dw, dtype)
+    twice = dw.clone()
+    layers.vocab_loss_grad(x, w, target, lse, dloss, twice, accumulate=True)
+    assert torch.equal(twice, dw + dw)
+
+
+def test_a_teachers_largest_logits(torch):
+    """Logits near the ends of fp32, which no temperature may carry beyond them."""
+    from paper_1805_07891_amd import layers
+    x, w, _, _ = _inputs(torch, 4, 48, 200, torch.float32)
+    index = torch.tensor([[3, 4], [5, 6], [7, -1], [8, 9]], device="cuda")
+    logits = torch.tensor([[3e38, 3e38], [-3e38, 3e38], [-3e38, 1.0], [-3e38, -3e38]], device="cuda")
+    for t in (1e-3, 0.5, 2.0):
+        # the same distributions from logits of ordinary size
+        plain = torch.tensor([[0.0, 0.0], [-1e4, 0.0], [0.0, 0.0], [0.0, 0.0]], device="cuda")
+        d = _definition(torch, x, w, index, plain, t, None)
+        loss, lse = layers.distill_loss(x, w, index, logits, t)
+        _check_loss(d, loss, lse)
+        dw = torch.empty(200, 48, device="cuda")
+        dx = layers.distill_loss_grad(x, w, index, logits, t, lse, None, dw)
+        _check_grad(torch, d, dx, dw, torch.float32)
+
+
 def test_no_live_rows_and_no_rows(torch):
     from paper_1805_07891_amd import layers
     x, w, target, dloss = _inputs(torch, 40, 64, 300, torch.bfloat16)
@@ -365,6 +433,44 @@ def test_captured_and_replayed(torch):
             torch.cuda.synchronize()
             for a, b in zip(got, (el, edx, dw)):
                 assert torch.equal(a, b)
+
+
+def test_two_graphs_share_a_workspace(torch):
+    from paper_1805_07891_amd import layers
+    first = _inputs(torch, 150, 72, 900, torch.float32)
+    second = _inputs(torch, 90, 40, 700, torch.bfloat16, top=11, seed=2)
+    space = layers.vocab_workspace(*first[:2])
+    assert space.numel() >= layers.vocab_workspace(*second[:2], 11).numel()
+    dws = [torch.empty(900, 72, device="cuda"), torch.empty(700, 40, device="cuda")]
+
+    def cross_entropy():
+        x, w, target, dloss = first
+        loss, lse = layers.vocab_loss(x, w, target, workspace=space)
+        return loss, layers.vocab_loss_grad(x, w, target, lse, dloss, dws[0], workspace=space), dws[0]
+
+    def distill():
+        x, w, index, logits, dloss = second
+        loss, lse = layers.distill_loss(x, w, index, logits, 2.0, workspace=space)
+        return loss, layers.distill_loss_grad(x, w, index, logits, 2.0, lse, dloss, dws[1],
+                                              workspace=space), dws[1]
+
+    want = [[t.clone() for t in run()] for run in (cross_entropy, distill)]
+    graphs, got = [], []
+    for run in (cross_entropy, distill):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got.append(run())
+        graphs.append(graph)
+    for order in ((0, 1), (1, 0), (0, 1)):
+        for out in got:
+            for t in out:
+                t.fill_(7.0)
+        for i in order:
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert all(torch.equal(p, q) for p, q in zip(a, b))
+        assert torch.equal(cross_entropy()[0], want[0][0])
 
 
 def test_two_streams_at_once(torch):
