@@ -118,9 +118,11 @@ def _check_grad(torch, d, dx, dw, dtype, pieces=1):
 
 
 # (rows, columns, vocabulary): one of each, odd ones, rows and columns that end inside a
-# tile, and products of enough tiles for each of the tile shapes
+# tile, products of enough tiles for each of the tile shapes, and of a little more than a
+# whole round of tiles (of the logits, of dw, of dx)
 SHAPES = [(1, 8, 1), (1, 1, 3), (2, 64, 1000), (5, 40, 300), (64, 128, 257), (100, 100, 1000),
-          (257, 72, 513), (300, 512, 2000), (513, 203, 777), (1100, 96, 4100), (2100, 72, 8200)]
+          (257, 72, 513), (300, 512, 2000), (513, 203, 777), (1100, 96, 4100), (2100, 72, 8200),
+          (600, 1100, 13100), (13100, 1100, 600)]
 
 
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
