@@ -78,16 +78,18 @@ __device__ __forceinline__ bool is_entry(int64_t v, int64_t vocab, float logit) 
     return v >= 0 && v < vocab && logit != -__builtin_huge_valf();
 }
 
-// words: top floats and top ints a wave.  The temperature divides what is left of
+// words: as many ints and floats a wave as entries, in whole fours.  The temperature divides what is left of
 // a logit below the largest, so that no logit is too large for it.
 __device__ __forceinline__ void prepare_teacher(const TeacherArgs& a, int block, float* words) {
     const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) / 64, top = a.top;
     const int64_t i = int64_t(block) * 4 + wave;
     if (i >= a.rows) return;
-    float* const val = words + 2 * top * wave;
-    int* const idx = reinterpret_cast<int*>(val + top);
+    const int whole = (top + 3) / 4 * 4;
+    int* const idx = reinterpret_cast<int*>(words) + 2 * whole * wave;
+    float* const val = reinterpret_cast<float*>(idx + whole);
     const float inv = 1.0f / a.temperature, low = -__builtin_huge_valf();
     float most = low;
+    if (lane < whole - top) idx[top + lane] = -1;
     for (int k = lane; k < top; k += 64) {
         const int64_t t = a.entry[i * top + k];
         const float l = a.logit[i * top + k];
@@ -114,12 +116,18 @@ __device__ __forceinline__ void prepare_teacher(const TeacherArgs& a, int block,
         float q = val[k];
         if (mine >= 0) {
             bool again = false;
-            q = 0.0f;
-#pragma unroll 8
-            for (int m = 0; m < top; ++m) {
-                const bool same = idx[m] == mine;
-                if (same) q += val[m];
-                again |= same && m < k;
+            typedef int i32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll 4
+            for (int m = 0; m < whole; m += 4) {
+                const i32x4 four = *reinterpret_cast<const i32x4*>(idx + m);
+                const bool same[4] = {four[0] == mine, four[1] == mine, four[2] == mine, four[3] == mine};
+                if (same[0] | same[1] | same[2] | same[3])
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (same[e] && m + e != k) {
+                            q += val[m + e];
+                            again |= m + e < k;
+                        }
             }
             if (again) mine = -1;
         }
@@ -434,6 +442,9 @@ struct Logits {
     const float* scale_w;   // [piece]; null: 1
     const int64_t* target;  // [rows]; null: a teacher's entries
     int64_t first;          // the piece's first vocabulary row
+    const int* index;       // the teacher's entries, [rows][top]
+    int top;
+    float* pick;            // [rows], or [rows][top]: the logits of targets (forward) or entries
 };
 
 // A row's target as a row of w in this piece, or -1.
@@ -443,14 +454,64 @@ __device__ __forceinline__ int target_of(const Logits& l, int row) {
     return v >= 0 && v < l.vocab ? int(v) : -1;
 }
 
+// The lane, found where it is asked for: what is computed from it is not moved ahead of
+// the product's loop, where it would take registers (or be spilled).
+__device__ __forceinline__ int lane_here() {
+    int lane = int(threadIdx.x) & 63;
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
+// The logits of a teacher's entries, by a wave that has those of 32 rows and N entries from
+// `row0` and `v0` on in LDS: value(row, entry).  They come from the product itself, not
+// from dot products of their own, because where softmax is near 1 an error of an entry's logit that
+// lse does not share stays whole in softmax - q (fp32 gradients were 4e-6 off instead of 1e-6).
+// Every tile looks through all of its rows' entries, which its die's L2 holds.
+template <int N, typename V>
+__device__ __forceinline__ void pick_entries(const Logits& l, int row0, int v0, V value) {
+    typedef int i32x4 __attribute__((ext_vector_type(4)));
+    constexpr int kLoads = 2;
+    const int lane = lane_here();
+    const int count = min(32, l.rows - row0) * l.top, last = (count - 1) / 4;
+    const int* const from = l.index + int64_t(row0) * l.top;  // 16-byte aligned, as is the array's end
+    float* const to = l.pick + int64_t(row0) * l.top;
+    const int base = int(l.first) + v0;
+    const unsigned n = unsigned(min(N, l.vocab - v0));
+    const float rows = 1.0f / float(l.top);  // (at < 2^15: never within its error of a whole number)
+    i32x4 r[kLoads], next[kLoads];
+    auto load = [&](int u, i32x4 (&to)[kLoads]) {
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k)
+            to[k] = *reinterpret_cast<const i32x4*>(from + min(u / 4 + k * 64 + lane, last) * 4);
+    };
+    if (count > 0) load(0, next);
+    for (int u = 0; u < count; u += kLoads * 256) {
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) r[k] = next[k];
+        load(u + kLoads * 256, next);
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+            unsigned v[4];  // (-1 is beyond any)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = unsigned(r[k][e] - base);
+            if (min(min(v[0], v[1]), min(v[2], v[3])) >= n) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int at = u + (k * 64 + lane) * 4 + e;
+                if (v[e] < n && at < count)
+                    to[at] = value(int((float(at) + 0.5f) * rows), int(v[e]));
+            }
+        }
+    }
+}
+
 struct ForwardOut {
     f32x2* part;  // [blocks of 32 WR vocabulary rows][rows]: an exponent n, sum of exp(z) 2^-n
     int first_block;
-    float* pick;  // [rows]: the targets' logits
 };
 
-// How logits come from the product: as they are; by the temperature; and, of
-// fp32 types, by the rows' scales too.
+// How logits come from the product: as they are (of targets); by a teacher's temperature;
+// and, of fp32 types, by the rows' scales too.
 enum Scaling { kPlain = 0, kTemperature = 1, kScaledRows = 2 };
 
 // R is w, C is x: a lane has one row of x and, in registers, entries of the
@@ -508,7 +569,30 @@ __global__ __launch_bounds__(kProductThreads) void logits_forward(Product p, Log
                         z = acc[i][j][r];
                         mine = true;
                     }
-            if (mine) out.pick[row] = z;
+            if (mine) l.pick[row] = z;
+        }
+        if (SCALING != kPlain && l.index) {
+            // [32 rows][32 WR entries], four entries a piece, places changed by row
+            constexpr int kPieces = WR * 8;
+            char* const part = lds + wave * (WR * 32 * 32 * 4);
+            const int lane = lane_here(), half = lane >> 5;
+            auto place_z = [](int row, int piece) {
+                return (row * kPieces + (piece ^ (row & (kPieces - 1)))) * 16;
+            };
+#pragma unroll
+            for (int i = 0; i < WR; ++i)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    f32x4 z;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[e] = acc[i][j][g * 4 + e];
+                    *reinterpret_cast<f32x4*>(part + place_z(lane & 31, i * 8 + g * 2 + half)) = z;
+                }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // other lanes of the wave read them
+            pick_entries<WR * 32>(l, i0 + j * 32, v0, [&](int row, int v) {
+                return *reinterpret_cast<const float*>(part + place_z(row, v / 4) + v % 4 * 4);
+            });
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
         f32x2 part;
         auto reduce = [&](auto is_cut) {
@@ -546,23 +630,20 @@ __global__ __launch_bounds__(kProductThreads) void logits_forward(Product p, Log
     }
 }
 
-// The logits of a teacher's entries, as the products above compute them: PAIRS (row,
+// The same for tiles of 256 x 256, whose epilogue has no registers for it: PAIRS (row,
 // entry) pairs a wave, rows of w gathered, of which the matrix instructions' 32 x 32
 // results give the diagonal.  The same instructions over the same k in the
-// same order give the same bits, and that matters: where softmax is near 1, an
-// error of the entry's logit that lse does not share stays whole in
-// softmax - q (with dot products of their own, fp32 gradients were 4e-6 off
-// instead of 1e-6).  Fragments come straight from memory, as no two pairs share
+// same order give the same bits as the product's.  Fragments come straight from memory, as no two pairs share
 // rows of w, those of the next AHEAD instructions while this many are done.
 template <typename T, int PAIRS, int AHEAD>
 __global__ __launch_bounds__(256) void target_logits(Operand x, Operand w, int k, int segments,
-                                                     Targets t, Logits l, float* pick) {
+                                                     Logits l) {
     typedef typename Frag<T>::type F;
     const int lane = int(threadIdx.x) & 63, n = lane & 31, half = lane >> 5;
     const int64_t pair = (int64_t(blockIdx.x) * 4 + threadIdx.x / 64) * PAIRS + n;
-    const int64_t row = pair / t.top;
+    const int64_t row = pair / l.top;
     int64_t v = -1;
-    if (n < PAIRS && row < l.rows) v = t.index[pair] - l.first;
+    if (n < PAIRS && row < l.rows) v = l.index[pair] - l.first;
     const bool in = v >= 0 && v < l.vocab;
     if (!__any(in)) return;
     const T* const xr = static_cast<const T*>(x.base) + (in ? row : 0) * x.ld + half * 8;
@@ -612,7 +693,7 @@ __global__ __launch_bounds__(256) void target_logits(Operand x, Operand w, int k
     for (int r = 0; r < 16; ++r) z = (n >> 3) * 4 + (n & 3) == r ? acc[r] : z;
     if (!in || half != (n >> 2 & 1)) return;
     const float sx = l.inv_temperature * (l.scale_x ? l.scale_x[row] : 1.0f);
-    pick[pair] = z * (sx * (l.scale_w ? l.scale_w[v] : 1.0f));
+    l.pick[pair] = z * (sx * (l.scale_w ? l.scale_w[v] : 1.0f));
 }
 
 constexpr int kFinishRows = 16;
@@ -722,7 +803,8 @@ template <typename T, int PLANES, int WANT, int WR, int WC, int STAGES>
 __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Logits l,
                                                                    BackwardOut out) {
     // a wave's part of LDS: what it needs of its rows, then 32 WR x 32 WC entries of 16 bits
-    constexpr int kAbout = WR * 32 * 20, kPart = kAbout + WR * WC * 2048;
+    // (or, before that, 32 rows' logits)
+    constexpr int kAbout = WR * 32 * 20, kPart = kAbout + (WR >= 2 ? WR * WC * 2048 : WC * 4096);
     constexpr int kStageBytes = TileShape<WR, WC>::kStageBytes * STAGES;
     __shared__ __attribute__((aligned(1024))) char lds[kStageBytes > 4 * kPart ? kStageBytes : 4 * kPart];
     const Place at = place(p);
@@ -767,6 +849,26 @@ __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Lo
             targets[u * 64 + lane] = target[u];
         }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // other lanes of the wave read them
+    if (WR < 4 && l.index && v0 < l.vocab) {
+        const int lane = lane_here(), half = lane >> 5;
+        float* const part = reinterpret_cast<float*>(lds + wave * kPart + kAbout);  // [32 rows][32 WC entries]
+#pragma unroll
+        for (int i = 0; i < WR; ++i) {
+#pragma unroll
+            for (int j = 0; j < WC; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    part[(r / 4 * 8 + half * 4 + r % 4) * (WC * 32) + j * 32 + (lane & 31)] = acc[i][j][r];
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // other lanes of the wave read them
+            const int row0 = i0 + i * 32;
+            pick_entries<WC * 32>(l, row0, v0, [&](int row, int v) {
+                float scale = l.inv_temperature;
+                if (PLANES == 2) scale = scale * l.scale_x[row0 + row] * l.scale_w[v0 + v];
+                return part[row * (WC * 32) + v] * scale;
+            });
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+    }
     float sw[WC], cw[WC];
     uint32_t in[WC];
 #pragma unroll
@@ -1377,7 +1479,7 @@ hipError_t launch_prepare(const VocabArgs& a, const Layout& l, bool is_first, co
     const int blocks = teacher.blocks + x.blocks + w.blocks + rows.blocks;
     if (blocks == 0) return hipSuccess;
     hipLaunchKernelGGL(prepare<S>, dim3(unsigned(blocks)), dim3(256),
-                       teacher.blocks ? unsigned(a.top) * 32 : 0, stream, teacher, x, w, rows,
+                       teacher.blocks ? unsigned((a.top + 3) / 4 * 4) * 32 : 0, stream, teacher, x, w, rows,
                        targets_of(a, l), int(a.cols), l.packed_ld);
     return hipGetLastError();
 }
@@ -1415,7 +1517,7 @@ void logits_of(const VocabArgs& a, const Layout& l, const PieceAt& at, Operand* 
     p->k = int(up(a.cols, 8));
     p->segments = l.planes == 2 ? 3 : 1;
     *z = {int(a.rows), int(at.rows), 1.0f / a.temperature, l.scale_x, l.scale_w,
-          a.top ? nullptr : a.target, at.first};
+          a.top ? nullptr : a.target, at.first, l.index, a.top, l.pick};
 }
 
 // Of these the vocabulary's rows from `first` on.
@@ -1426,19 +1528,32 @@ Logits logits_from(Logits z, int64_t first, int64_t n) {
     return z;
 }
 
-// The logits of a teacher's entries in a piece.  Few pairs are spread over more
-// waves.
+// Whether the logits of a teacher's entries are gathered, or the product's epilogue has
+// them: of its own tiles it knows them for nothing but a look through their rows' entries.  Large tiles'
+// backward epilogue has no registers for that (loss and gradients of 4096 rows, 2048 columns, 65536 entries,
+// 32 of the teacher, bf16: 5.62 ms gathered, 5.78 without), in the forward pass measured rates decide:
+// the gathered bytes at 7 TB/s against 1.5 us and 0.1 an entry for each round of tiles.  E.g. of
+// that size 964 us gathered and 991 without for 1 entry, 1271 and 1132 for 128; 2048, 2048, 32768,
+// fp32, 128: 1287 and 849; 64, 1024, 16384, fp32, 64 (small tiles): 71 and 52.
+bool gathered_entries(int shape, const Logits& z, int cols, int segments, bool grad) {
+    if (!z.index || shape != kBig) return false;
+    if (grad) return true;
+    const int64_t blocks = tiles_of(shape, z.rows) * tiles_of(shape, z.vocab);
+    const float gather = kLaunchCost + float(z.rows) * float(z.top) * float(cols * segments) * 2.0f / 7e6f;
+    return gather < float((blocks + kUnits - 1) / kUnits) * (1.5f + 0.1f * float(z.top));
+}
+
+// Few pairs are spread over more waves.
 template <typename T>
-hipError_t pick_of(const VocabArgs& a, const Layout& l, const Operand& x, const Operand& w,
-                   const Product& p, const Logits& z, hipStream_t stream) {
-    if (a.top == 0) return hipSuccess;
-    const int64_t pairs = a.rows * a.top;
+hipError_t gather_entries(const Operand& x, const Operand& w, const Product& p, const Logits& z,
+                          hipStream_t stream) {
+    const int64_t pairs = int64_t(z.rows) * z.top;
     if (pairs < 4 * kUnits * 32)
         hipLaunchKernelGGL((target_logits<T, 8, 16>), dim3(unsigned((pairs + 31) / 32)), dim3(256), 0,
-                           stream, x, w, p.k, p.segments, targets_of(a, l), z, l.pick);
+                           stream, x, w, p.k, p.segments, z);
     else
         hipLaunchKernelGGL((target_logits<T, 32, 8>), dim3(unsigned((pairs + 127) / 128)), dim3(256), 0,
-                           stream, x, w, p.k, p.segments, targets_of(a, l), z, l.pick);
+                           stream, x, w, p.k, p.segments, z);
     return hipGetLastError();
 }
 
@@ -1458,16 +1573,20 @@ hipError_t loss_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
         e = each_part(l.logits_plan, at.rows, [&](int shape, int64_t first, int64_t n) {
             Product d = p;
             d.r = rows_of(p.r, first, n);
-            const Logits part = logits_from(z, first, n);
-            const ForwardOut o{l.part, blocks, l.pick};
+            Logits part = logits_from(z, first, n);
+            const ForwardOut o{l.part, blocks};
             const int block = kTileRows[shape] / 2;
             blocks += int((n + block - 1) / block);
+            if (gathered_entries(shape, part, d.k, d.segments, false)) {
+                const hipError_t g = gather_entries<T>(d.c, d.r, d, part, stream);
+                if (g != hipSuccess) return g;
+                part.index = nullptr;
+            }
             if constexpr (std::is_same<S, float>::value)
                 return run_forward<T, kScaledRows>(shape, d, part, o, stream);
-            return a.temperature == 1.0f ? run_forward<T, kPlain>(shape, d, part, o, stream)
-                                         : run_forward<T, kTemperature>(shape, d, part, o, stream);
+            return a.top == 0 ? run_forward<T, kPlain>(shape, d, part, o, stream)
+                              : run_forward<T, kTemperature>(shape, d, part, o, stream);
         });
-        if (e == hipSuccess) e = pick_of<T>(a, l, p.c, p.r, p, z, stream);
     }
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(finish_loss, dim3(unsigned((a.rows + kFinishRows - 1) / kFinishRows)),
@@ -1517,12 +1636,15 @@ hipError_t grad_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
             BackwardOut to = o;
             if (a.dx) to.p = static_cast<T*>(o.p) + first;
             if (a.dw) to.q = o.q + first * o.ld_q;
+            if (gathered_entries(shape, part, d.k, d.segments, true)) {
+                const hipError_t g = gather_entries<T>(d.r, d.c, d, part, stream);
+                if (g != hipSuccess) return g;
+            }
             return !a.dw   ? run_backward<T, PLANES, 1>(shape, d, part, to, stream)
                    : !a.dx ? run_backward<T, PLANES, 2>(shape, d, part, to, stream)
                            : run_backward<T, PLANES, 3>(shape, d, part, to, stream);
         });
         if (e != hipSuccess) return e;
-        if ((e = pick_of<T>(a, l, p.r, p.c, p, z, stream)) != hipSuccess) return e;
         if (a.top) {
             const int64_t entries = a.rows * a.top;
             hipLaunchKernelGGL((take_targets<T, PLANES>), dim3(unsigned((entries + 255) / 256)),
