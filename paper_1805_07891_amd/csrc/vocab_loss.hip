@@ -11,9 +11,10 @@
 //   G = g T (softmax(z) - q),   dx = G w,   dw = G^T x.
 //
 // Forward: each tile of the product leaves, for every row, a power of two and
-// the sum of exponentials of its part of the vocabulary relative to it, and the logits of the
-// targets in it; a second kernel joins them.  The 4 N V bytes of logits are
-// never written.  A teacher's entries have a kernel of their own.
+// the sum of exponentials of its part of the vocabulary relative to it, and the
+// logits of the targets in it; a second kernel joins them.  The 4 N V bytes of
+// logits are never written.  A teacher's many entries in large tiles may have a
+// kernel of their own.
 //
 // Backward: the logits are computed again, a piece of the vocabulary at a
 // time (as much as the workspace takes), and softmax(z) goes to the
