@@ -352,11 +352,19 @@ __device__ __forceinline__ void describe_rows(const RowsArgs& a, const Targets& 
     leave_largest(most, a.largest, block);
 }
 
+// Words that a product's blocks count in, by one block.
+struct ClearArgs {
+    int blocks;  // 0: nothing to clear
+    int* words;
+    int count;
+};
+
 // All of these in one launch, a run of blocks each: the teacher's first, which
 // take longest.
 template <typename T>
 __global__ __launch_bounds__(256) void prepare(TeacherArgs teacher, PackArgs x, PackArgs w,
-                                               RowsArgs rows, Targets t, int cols, int64_t ld) {
+                                               RowsArgs rows, ClearArgs clear, Targets t, int cols,
+                                               int64_t ld) {
     extern __shared__ float words[];
     int block = int(blockIdx.x);
     if (block < teacher.blocks) return prepare_teacher(teacher, block, words);
@@ -364,7 +372,9 @@ __global__ __launch_bounds__(256) void prepare(TeacherArgs teacher, PackArgs x, 
     if (block < x.blocks) return pack_rows<T>(x, block, cols, ld);
     block -= x.blocks;
     if (block < w.blocks) return pack_rows<T>(w, block, cols, ld);
-    describe_rows<T>(rows, t, teacher, block - w.blocks, cols);
+    block -= w.blocks;
+    if (block < rows.blocks) return describe_rows<T>(rows, t, teacher, block, cols);
+    for (int i = int(threadIdx.x); i < clear.count; i += 256) clear.words[i] = 0;
 }
 
 // dst[c][r] = src[r][c] for columns c < cols, and zero for rows up to ld (a
@@ -446,6 +456,8 @@ struct Logits {
     const int* index;       // the teacher's entries, [rows][top]
     int top;
     float* pick;            // [rows], or [rows][top]: the logits of targets (forward) or entries
+    uint64_t* parts;        // [tiles][splits][8][256 threads], of 64 x 64 tiles; null: no splits
+    int* arrived;           // [tiles]: blocks that have left their part
 };
 
 // A row's target as a row of w in this piece, or -1.
@@ -506,6 +518,47 @@ __device__ __forceinline__ void pick_entries(const Logits& l, int row0, int v0, 
     }
 }
 
+// Adds the parts of a tile's k loop.  Each block leaves its part in memory and counts
+// itself, and the last one adds all of them, in order (the same bits whichever
+// block that is), and goes on with the tile: true.  Nobody waits for another.
+// The blocks may be on dies with L2s of their own: parts are written and read as relaxed
+// atomics of the device's scope, which go past L2, and a block counts itself when its
+// writes have arrived.  (Fences instead write back the whole L2, a thousand times: 40 us for 256 blocks.)
+__device__ __forceinline__ bool add_parts(const Product& p, const Place& at, const Logits& l,
+                                          f32x16 (&acc)[1][1]) {
+    __shared__ int before;
+    const int tile = at.r * p.tiles_c + at.c;
+    uint64_t* const first = l.parts + int64_t(tile) * p.splits * 2048 + threadIdx.x;
+#pragma unroll
+    for (int g = 0; g < 8; ++g) {
+        const f32x2 v = {acc[0][0][g * 2], acc[0][0][g * 2 + 1]};
+        __hip_atomic_store(first + at.split * 2048 + g * 256, __builtin_bit_cast(uint64_t, v),
+                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0)
+        before = __hip_atomic_fetch_add(l.arrived + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (before != p.splits - 1) return false;
+    acc[0][0] = f32x16{};
+#pragma unroll 2
+    for (int s = 0; s < p.splits; ++s) {
+        uint64_t part[8];
+#pragma unroll
+        for (int g = 0; g < 8; ++g)
+            part[g] = __hip_atomic_load(first + s * 2048 + g * 256, __ATOMIC_RELAXED,
+                                        __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+            const f32x2 v = __builtin_bit_cast(f32x2, part[g]);
+            acc[0][0][g * 2] += v.x;
+            acc[0][0][g * 2 + 1] += v.y;
+        }
+    }
+    return true;
+}
+
 struct ForwardOut {
     f32x2* part;  // [blocks of 32 WR vocabulary rows][rows]: an exponent n, sum of exp(z) 2^-n
     int first_block;
@@ -548,6 +601,8 @@ __global__ __launch_bounds__(kProductThreads) void logits_forward(Product p, Log
                     sw[i][g] = *reinterpret_cast<const f32x4*>(l.scale_w + v0 + i * 32 + g * 8 + half * 4);
     });
 
+    if constexpr (WR == 1)
+        if (p.splits > 1 && !add_parts(p, at, l, acc)) return;
     const float low = -__builtin_huge_valf();
     if (v0 >= l.vocab) return;
 #pragma unroll
@@ -841,6 +896,8 @@ __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Lo
         }
     });
 
+    if constexpr (WR == 1)
+        if (p.splits > 1 && !add_parts(p, at, l, acc)) return;
     f32x4* const about = reinterpret_cast<f32x4*>(lds + wave * kPart);
     int* const targets = reinterpret_cast<int*>(about + WR * 32);
 #pragma unroll
@@ -1218,6 +1275,7 @@ constexpr int kStages[] = {4, 4, 4};
 constexpr int kUnits = 256;  // compute units
 constexpr int kMostSplits = 32;
 constexpr float kLaunchCost = 4.0f, kJoinBytes = 4e6f;  // us of one more launch; bytes a us
+constexpr float kCountCost = 7.0f;  // us of parts that the last block adds
 
 // A product's first `main` rows of the dimension that can be cut in tiles of `shape`, the rest
 // in tiles of `tail`, each block one of `splits` parts of the k loop.
@@ -1232,8 +1290,12 @@ float rounds_cost(int shape, int64_t blocks, float steps) {
 
 int64_t tiles_of(int shape, int64_t n) { return (n + kTileRows[shape] - 1) / kTileRows[shape]; }
 
+// How parts of the k loop become a sum: not at all; by a kernel; or (64 x 64 tiles, in
+// one round) by the tile's last block.
+enum Parts { kOne, kJoined, kCounted };
+
 // The cheapest plan for a product of `whole` by `cut` rows over `steps` x 64 of k.
-Plan choose_plan(int64_t whole, int64_t cut, int64_t steps, bool may_split) {
+Plan choose_plan(int64_t whole, int64_t cut, int64_t steps, Parts parts) {
     Plan best;
     float least = __builtin_huge_valf();
     auto consider = [&](float cost, int shape, int tail, int splits, int64_t main) {
@@ -1246,12 +1308,17 @@ Plan choose_plan(int64_t whole, int64_t cut, int64_t steps, bool may_split) {
     };
     for (int shape = kBig; shape <= kSmall; ++shape) {
         const int64_t across = tiles_of(shape, whole), tiles = across * tiles_of(shape, cut);
-        for (int splits = 1; splits <= (may_split ? kMostSplits : 1); splits *= 2) {
-            if (splits > 1 && (tiles * splits > 2 * kUnits || steps < 4 * splits)) break;
+        const int most = parts == kJoined ? kMostSplits : parts == kCounted && shape == kSmall ? 8 : 1;
+        for (int splits = 1; splits <= most; splits *= 2) {
+            const int rounds = parts == kJoined ? 2 : 1;
+            if (splits > 1 && (tiles * splits > rounds * kUnits || steps < 4 * splits)) break;
             float cost = rounds_cost(shape, tiles * splits, float(steps) / float(splits));
-            // parts are written and read in fp32, and joined by a kernel
+            // parts are written and read in fp32 (counted ones: 256 x 2048 x 1000, fp32, 34.7 -> 27.2
+            // us a loss; bf16, a third of the steps, 15.4 -> 18.2 and so left whole; 1 x 8192 x
+            // 200, fp32, 83 -> 33)
             if (splits > 1)
-                cost += kLaunchCost + float(splits) * float(whole) * float(cut) * 8.0f / kJoinBytes;
+                cost += (parts == kCounted ? kCountCost : kLaunchCost) +
+                        float(splits) * float(whole) * float(cut) * 8.0f / kJoinBytes;
             consider(cost, shape, shape, splits, cut);
         }
         // whole rounds of these tiles, and what is left in smaller ones (1023 rows, 2047
@@ -1362,6 +1429,9 @@ struct Layout {
     int planes;         // 2: fp32
     Plan logits_plan, dx_plan, dw_plan;  // cut by vocabulary, rows and vocabulary
     int64_t blocks;     // of the vocabulary, in a piece: sums that a row leaves
+    int counted;
+    uint64_t* parts;
+    int* arrived;
     // parts
     int *index, *teacher_alive, *alive, *row_exponent, *w_exponent, *largest, *largest_w;
     float *weight, *factor, *entropy, *pick, *scale_x, *scale_w, *part_x, *part_w;
@@ -1388,9 +1458,15 @@ Layout lay_out(const VocabArgs& a, bool grad, int64_t piece, Arena* arena) {
     const bool dx = grad && a.dx, dw = grad && a.dw;
     const int64_t most = std::min(piece, a.vocab);  // rows of w in a piece
     const int64_t steps = (a.cols + 63) / 64;
-    l.logits_plan = choose_plan(a.rows, most, steps * (l.planes == 2 ? 3 : 1), false);
+    l.logits_plan = choose_plan(a.rows, most, steps * (l.planes == 2 ? 3 : 1), kCounted);
     l.blocks = 2 * (tiles_of(l.logits_plan.shape, l.logits_plan.main) +
                     tiles_of(l.logits_plan.tail, most - l.logits_plan.main));
+
+    const int64_t counted =  // tiles of the logits' product that are done in parts
+        l.logits_plan.splits > 1 ? tiles_of(kSmall, a.rows) * tiles_of(kSmall, most) : 0;
+    l.counted = int(counted);
+    l.parts = arena->take<uint64_t>(counted * l.logits_plan.splits * 2048, counted > 0);
+    l.arrived = arena->take<int>(counted, counted > 0);
 
     l.ld_p = piece + kPad;
     l.index = arena->take<int>(entries, a.top > 0);
@@ -1414,12 +1490,12 @@ Layout lay_out(const VocabArgs& a, bool grad, int64_t piece, Arena* arena) {
     l.q = arena->take<fp16>(2 * piece * l.rows_ld, dw);
     l.xt = arena->take<char>(l.planes * a.cols * l.rows_ld * 2, dw);
     if (dx) {
-        l.dx_plan = choose_plan(a.cols, a.rows, (most + 63) / 64 * (l.planes == 2 ? 3 : 1), true);
+        l.dx_plan = choose_plan(a.cols, a.rows, (most + 63) / 64 * (l.planes == 2 ? 3 : 1), kJoined);
         l.part_x = arena->take<float>(int64_t(l.dx_plan.splits) * a.rows * a.cols,
                                       l.dx_plan.splits > 1 || l.pieces > 1);
     }
     if (dw) {
-        l.dw_plan = choose_plan(a.cols, most, (a.rows + 63) / 64 * (l.planes == 2 ? 3 : 2), true);
+        l.dw_plan = choose_plan(a.cols, most, (a.rows + 63) / 64 * (l.planes == 2 ? 3 : 2), kJoined);
         l.part_w = arena->take<float>(int64_t(l.dw_plan.splits) * most * a.cols,
                                       l.dw_plan.splits > 1);
     }
@@ -1477,11 +1553,12 @@ hipError_t launch_prepare(const VocabArgs& a, const Layout& l, bool is_first, co
     if (a.top)
         teacher = {is_first ? int((a.rows + 3) / 4) : 0, a.rows, a.vocab, a.top, a.target, a.logit,
                    a.temperature, l.index, l.weight, l.teacher_alive, l.entropy};
-    const int blocks = teacher.blocks + x.blocks + w.blocks + rows.blocks;
+    const ClearArgs clear{l.counted > 0, l.arrived, l.counted};
+    const int blocks = teacher.blocks + x.blocks + w.blocks + rows.blocks + clear.blocks;
     if (blocks == 0) return hipSuccess;
     hipLaunchKernelGGL(prepare<S>, dim3(unsigned(blocks)), dim3(256),
                        teacher.blocks ? unsigned((a.top + 3) / 4 * 4) * 32 : 0, stream, teacher, x, w, rows,
-                       targets_of(a, l), int(a.cols), l.packed_ld);
+                       clear, targets_of(a, l), int(a.cols), l.packed_ld);
     return hipGetLastError();
 }
 
@@ -1517,8 +1594,10 @@ void logits_of(const VocabArgs& a, const Layout& l, const PieceAt& at, Operand* 
         *x = {a.x, a.x_stride, 0, int(a.rows)};
     p->k = int(up(a.cols, 8));
     p->segments = l.planes == 2 ? 3 : 1;
+    p->splits = l.logits_plan.splits;
     *z = {int(a.rows), int(at.rows), 1.0f / a.temperature, l.scale_x, l.scale_w,
-          a.top ? nullptr : a.target, at.first, l.index, a.top, l.pick};
+          a.top ? nullptr : a.target, at.first, l.index, a.top, l.pick, l.parts,
+          l.arrived};
 }
 
 // Of these the vocabulary's rows from `first` on.
