@@ -506,8 +506,9 @@ int phub_vocab_bytes(int type, int64_t rows, int64_t cols, int64_t vocab, const 
  * in x.
  * Products of fp32 matrices are made of two 16-bit parts of each value: right
  * to about 2^-23 of each product, and to 2^-38 of the largest values of the two rows
- * where others are much smaller.  A value that is not finite makes the logits
- * of its row (or, in w, of its entry) not finite.
+ * where others are much smaller; the largest value of a row of x times that of
+ * a row of w has to stay below 2^127.  A value that is not finite makes the
+ * logits of its row (or, in w, of its entry) not finite.
  */
 int phub_vocab_loss(int type, int64_t rows, int64_t cols, int64_t vocab, const void *x,
                     int64_t x_stride, const void *w, int64_t w_stride, const int64_t *target,

@@ -170,7 +170,9 @@ def _sizes(x, w):
 
 
 def _teacher(x, index, logits, temperature):
-    pi, _ = _matrix("index", index, (x.shape[0], index.shape[-1]), torch.int64, x.device)
+    pi, _ = _matrix("index", index, None, torch.int64, x.device)
+    if index.shape[0] != x.shape[0]:
+        raise ValueError(f"index has {index.shape[0]} rows, x {x.shape[0]}")
     pl, _ = _matrix("logits", logits, index.shape, _FP32, x.device)
     if not index.is_contiguous() or not logits.is_contiguous():
         raise ValueError("index and logits must be contiguous")
