@@ -761,7 +761,7 @@ __global__ __launch_bounds__(1024) void finish_loss(const f32x2* part, int block
                                                     const float* entropy, float temperature,
                                                     float* loss, float* lse) {
     __shared__ f32x2 words[64][kFinishRows];
-    __shared__ float ends[kFinishRows];
+    __shared__ f32x2 ends[kFinishRows];
     const int in = int(threadIdx.x) % kFinishRows, group = int(threadIdx.x) / kFinishRows;
     const int64_t first = int64_t(blockIdx.x) * kFinishRows;
     // a sum of 0 has no reference (-inf logits alone)
@@ -770,6 +770,11 @@ __global__ __launch_bounds__(1024) void finish_loss(const f32x2* part, int block
         if (a.y == 0.0f) return b;
         const float n = __builtin_fmaxf(a.x, b.x);
         return f32x2{n, a.y * __builtin_amdgcn_exp2f(a.x - n) + b.y * __builtin_amdgcn_exp2f(b.x - n)};
+    };
+    // n ln 2 + ln sum - z, in an order that leaves the loss of a row whose target has
+    // nearly all of the softmax (z near n ln 2) right to 2^-25, not to lse's last bit
+    auto above = [](f32x2 end, float z) {
+        return __builtin_fmaf(end.x, 0x1.62e42ep-1f, -z) + __builtin_fmaf(end.x, 0x1.efa39ep-25f, end.y);
     };
     f32x2 s = {0.0f, 0.0f};
     if (first + in < rows) {
@@ -785,24 +790,23 @@ __global__ __launch_bounds__(1024) void finish_loss(const f32x2* part, int block
     }
     if (group == 0 && first + in < rows) {
         const f32x2 all = words[0][in];
-        // n ln 2 + ln sum
-        const float end = __builtin_fmaf(all.x, 0x1.62e42ep-1f, __builtin_fmaf(all.x, 0x1.efa39ep-25f, logf(all.y)));
+        const f32x2 end = {all.x, logf(all.y)};
         ends[in] = end;
-        lse[first + in] = end;
+        lse[first + in] = above(end, 0.0f);
     }
     __syncthreads();
     const int wave = int(threadIdx.x) / 64, lane = int(threadIdx.x) & 63;
     const int64_t row = first + wave;
     if (row >= rows) return;
-    const float end = ends[wave];
+    const f32x2 end = ends[wave];
     float out = 0.0f;
     if (t.target) {
-        if (index_of(t, row, 0) >= 0) out = end - pick[row];
+        if (index_of(t, row, 0) >= 0) out = above(end, pick[row]);
     } else if (alive[row]) {
         for (int k = lane; k < t.top; k += 64) {
             const float q = t.weight[row * t.top + k];  // 0 where there is no entry
             // relative to lse, so that nothing large cancels
-            if (q != 0.0f) out = __builtin_fmaf(q, end - pick[row * t.top + k], out);
+            if (q != 0.0f) out = __builtin_fmaf(q, above(end, pick[row * t.top + k]), out);
         }
         out = temperature * temperature * (entropy[row] + wave_sum(out));
     }
