@@ -10,8 +10,8 @@
 //
 //   G = g T (softmax(z) - q),   dx = G w,   dw = G^T x.
 //
-// Forward: each tile of the product leaves, for every row, a power of two and
-// the sum of exponentials of its part of the vocabulary relative to it, and the
+// Forward: each tile of the product leaves, for every row, the largest logit of
+// its part of the vocabulary and the sum of exponentials relative to it, and the
 // logits of the targets in it; a second kernel joins them.  The 4 N V bytes of
 // logits are never written.  A teacher's many entries in large tiles may have a
 // kernel of their own.
@@ -560,7 +560,7 @@ __device__ __forceinline__ bool add_parts(const Product& p, const Place& at, con
 }
 
 struct ForwardOut {
-    f32x2* part;  // [blocks of 32 WR vocabulary rows][rows]: an exponent n, sum of exp(z) 2^-n
+    f32x2* part;  // [blocks of 32 WR vocabulary rows][rows]: the largest logit m, sum of exp(z - m)
     int first_block;
 };
 
@@ -663,18 +663,20 @@ __global__ __launch_bounds__(kProductThreads) void logits_forward(Product p, Log
                 for (int r = 0; r < 16; ++r)
                     if (in(i, r)) most = __builtin_fmaxf(most, acc[i][j][r]);
             most = __builtin_fmaxf(most, __shfl_xor(most, 32));
-            // relative to a power of two, so that the reference is exact: the
-            // argument of exp2 is rounded once
-            const float n = most == low ? 0.0f : __builtin_rintf(most * kLog2e);
+            // z - m first, then its multiple: the largest one's term is 1 whatever its size,
+            // and the others are off by as much of their distance as fp32 rounds away.  (One
+            // fma of z, kLog2e and a power of two is an instruction less, but kLog2e's last bits
+            // then count with all of z: losses of -6.6e-7 for a logit of 50, NaN from 1e10 on.)
+            const float m = most == low ? 0.0f : most;
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < WR; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if (in(i, r))
-                        sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][r], kLog2e, -n));
+                        sum += __builtin_amdgcn_exp2f((acc[i][j][r] - m) * kLog2e);
             sum += __shfl_xor(sum, 32);
-            part = f32x2{n, sum};
+            part = f32x2{m, sum};
         };
         // (only the last blocks of a piece are cut)
         if (v0 + WR * 32 > l.vocab)
@@ -768,14 +770,13 @@ __global__ __launch_bounds__(1024) void finish_loss(const f32x2* part, int block
     auto join = [](f32x2 a, f32x2 b) {
         if (b.y == 0.0f) return a;
         if (a.y == 0.0f) return b;
-        const float n = __builtin_fmaxf(a.x, b.x);
-        return f32x2{n, a.y * __builtin_amdgcn_exp2f(a.x - n) + b.y * __builtin_amdgcn_exp2f(b.x - n)};
+        const float m = __builtin_fmaxf(a.x, b.x);
+        return f32x2{m, a.y * __builtin_amdgcn_exp2f((a.x - m) * kLog2e) +
+                            b.y * __builtin_amdgcn_exp2f((b.x - m) * kLog2e)};
     };
-    // n ln 2 + ln sum - z, in an order that leaves the loss of a row whose target has
-    // nearly all of the softmax (z near n ln 2) right to 2^-25, not to lse's last bit
-    auto above = [](f32x2 end, float z) {
-        return __builtin_fmaf(end.x, 0x1.62e42ep-1f, -z) + __builtin_fmaf(end.x, 0x1.efa39ep-25f, end.y);
-    };
+    // lse - z, never below 0 (the largest logit's own term makes the sum 1 or more), and where the
+    // target has nearly all of the softmax right to the sum's last bit, not to lse's
+    auto above = [](f32x2 end, float z) { return (end.x - z) + end.y; };
     f32x2 s = {0.0f, 0.0f};
     if (first + in < rows) {
 #pragma unroll 4
@@ -792,7 +793,7 @@ __global__ __launch_bounds__(1024) void finish_loss(const f32x2* part, int block
         const f32x2 all = words[0][in];
         const f32x2 end = {all.x, logf(all.y)};
         ends[in] = end;
-        lse[first + in] = above(end, 0.0f);
+        lse[first + in] = end.x + end.y;
     }
     __syncthreads();
     const int wave = int(threadIdx.x) / 64, lane = int(threadIdx.x) & 63;
