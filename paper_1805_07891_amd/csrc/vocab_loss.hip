@@ -41,7 +41,8 @@ namespace phub {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
-constexpr int kNoExponent = -100000;  // of a row of zeros
+constexpr int kNoExponent = -100000;  // of no row at all
+constexpr int kLeastExponent = -100;  // of a row: smaller values, and zeros, count as this large
 
 // ------------------------------------------------------------ the targets
 
@@ -146,10 +147,13 @@ __device__ __forceinline__ void prepare_teacher(const TeacherArgs& a, int block,
 
 // ------------------------------------------- operands as the product reads them
 
-// e with |v| < 2^e (0 for 0, inf and NaN, which no scale changes).
+// e with |v| < 2^e.  A row of zeros has the least: it takes part in the largest exponent of
+// all rows, at which the others' factors are held, and what it is multiplied with may
+// vanish.  0 for inf and NaN: what those reach is not finite at any scale.
 __device__ __forceinline__ int exponent_of(float most) {
-    if (!(most > 0.0f) || most == __builtin_huge_valf()) return 0;
-    return max(-100, __builtin_amdgcn_frexp_expf(most));
+    if (most == 0.0f) return kLeastExponent;
+    if (!(most < __builtin_huge_valf())) return 0;
+    return max(kLeastExponent, __builtin_amdgcn_frexp_expf(most));
 }
 
 // A product as the fp32 value that it rounds to.  Without this the compiler
@@ -938,7 +942,8 @@ __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Lo
     for (int j = 0; j < WC; ++j) {
         const int v = v0 + j * 32 + (lane & 31);
         in[j] = v < l.vocab ? ~0u : 0u;
-        sw[j] = PLANES == 2 && in[j] ? l.scale_w[v] : 1.0f;
+        // (0, not 1, for an entry that is not there: 2^28 less the largest may be past fp32)
+        sw[j] = PLANES == 2 && in[j] ? l.scale_w[v] : 0.0f;
         // P's scale: into fp16's range, and fp32's rows of w to the piece's largest
         cw[j] = PLANES == 2                       ? __builtin_amdgcn_ldexpf(sw[j], 28 - largest_w)
                 : std::is_same<T, fp16>::value ? 16384.0f
