@@ -568,6 +568,12 @@ struct ForwardOut {
     int first_block;
 };
 
+// The rows' scales are powers of two, multiplied with each other before the
+// temperature is: either alone may be so large that divided by it it is beyond fp32.
+__device__ __forceinline__ float scale_of(float scale_x, float scale_w, float inv_temperature) {
+    return scale_x * scale_w * inv_temperature;
+}
+
 // How logits come from the product: as they are (of targets); by a teacher's temperature;
 // and, of fp32 types, by the rows' scales too.
 enum Scaling { kPlain = 0, kTemperature = 1, kScaledRows = 2 };
@@ -593,8 +599,7 @@ __global__ __launch_bounds__(kProductThreads) void logits_forward(Product p, Log
         for (int j = 0; j < WC; ++j) {
             const int row = i0 + j * 32 + (lane & 31), v = target_of(l, row) - v0;
             target[j] = v < WR * 32 ? v : -1;
-            sx[j] = l.inv_temperature;
-            if (SCALING == kScaledRows && row < l.rows) sx[j] *= l.scale_x[row];
+            sx[j] = SCALING == kScaledRows && row < l.rows ? l.scale_x[row] : 1.0f;
         }
         // (the scales' array goes on to the end of a tile)
         if constexpr (SCALING == kScaledRows)
@@ -617,7 +622,9 @@ __global__ __launch_bounds__(kProductThreads) void logits_forward(Product p, Log
             for (int i = 0; i < WR; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    acc[i][j][r] *= SCALING == kScaledRows ? sx[j] * sw[i][r / 4][r % 4] : sx[j];
+                    acc[i][j][r] *= SCALING == kScaledRows
+                                        ? scale_of(sx[j], sw[i][r / 4][r % 4], l.inv_temperature)
+                                        : l.inv_temperature;
         if (__any(target[j] >= 0)) {
             float z = 0.0f;
             bool mine = false;
@@ -754,8 +761,8 @@ __global__ __launch_bounds__(256) void target_logits(Operand x, Operand w, int k
 #pragma unroll
     for (int r = 0; r < 16; ++r) z = (n >> 3) * 4 + (n & 3) == r ? acc[r] : z;
     if (!in || half != (n >> 2 & 1)) return;
-    const float sx = l.inv_temperature * (l.scale_x ? l.scale_x[row] : 1.0f);
-    l.pick[pair] = z * (sx * (l.scale_w ? l.scale_w[v] : 1.0f));
+    l.pick[pair] = z * scale_of(l.scale_x ? l.scale_x[row] : 1.0f, l.scale_w ? l.scale_w[v] : 1.0f,
+                                l.inv_temperature);
 }
 
 constexpr int kFinishRows = 16;
@@ -878,8 +885,8 @@ __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Lo
     const int half = lane >> 5, odd = lane & 1;
     const int i0 = (at.r * 2 + wave / 2) * WR * 32, v0 = (at.c * 2 + wave % 2) * WC * 32;
     constexpr bool want_p = WANT & 1, want_q = WANT & 2;
-    // the wave's rows, one or two a lane: lse, scale, factor of Q, whether it is
-    // alive; and its target among the wave's entries
+    // the wave's rows, one or two a lane: lse, scale (of fp32 types without the
+    // temperature's), factor of Q, whether it is alive; and its target among the wave's entries
     constexpr int kMine = (WR * 32 + 63) / 64;
     f32x4 mine[kMine];
     int target[kMine], largest_w = 0;
@@ -894,7 +901,7 @@ __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Lo
             mine[u] = f32x4{};
             if (have) {
                 mine[u].x = out.lse[row];
-                mine[u].y = l.inv_temperature * (PLANES == 2 ? l.scale_x[row] : 1.0f);
+                mine[u].y = PLANES == 2 ? l.scale_x[row] : l.inv_temperature;
                 if (want_q)
                     mine[u].z =
                         __builtin_amdgcn_ldexpf(out.factor[row], out.row_exponent[row] - largest + 14);
@@ -929,8 +936,9 @@ __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Lo
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // other lanes of the wave read them
             const int row0 = i0 + i * 32;
             pick_entries<WC * 32>(l, row0, v0, [&](int row, int v) {
-                float scale = l.inv_temperature;
-                if (PLANES == 2) scale = scale * l.scale_x[row0 + row] * l.scale_w[v0 + v];
+                const float scale =
+                    PLANES == 2 ? scale_of(l.scale_x[row0 + row], l.scale_w[v0 + v], l.inv_temperature)
+                                : l.inv_temperature;
                 return part[row * (WC * 32) + v] * scale;
             });
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -989,8 +997,9 @@ __global__ __launch_bounds__(kProductThreads) void logits_backward(Product p, Lo
                 f32x4 y;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float d = __builtin_fmaf(acc[i][j][g * 4 + e],
-                                                   PLANES == 2 ? row[e].y * sw[j] : row[e].y, -row[e].x);
+                    const float d = __builtin_fmaf(
+                        acc[i][j][g * 4 + e],
+                        PLANES == 2 ? scale_of(row[e].y, sw[j], l.inv_temperature) : row[e].y, -row[e].x);
                     // a row or entry that is not there, or not alive, is 0 whatever it held
                     const float s = __builtin_amdgcn_exp2f(d * kLog2e);
                     const float mask = row[e].w;  // (bit_cast of a vector's element takes the first)
