@@ -482,7 +482,8 @@ int phub_layer_norm_grad(int type, int64_t rows, int64_t cols, const void *dy, i
  * phub_vocab_bytes - bytes of workspace for the four functions below:
  * *least, the fewest that a call takes, and *best, as many as it has use for
  * (either may be NULL).  With fewer than *best the vocabulary is done in more
- * pieces.
+ * pieces: slower, and sums over it are added in another order.  What the
+ * backward pass takes is enough for the forward pass of the same sizes.
  *   top   the teacher's entries a row, 0 for phub_vocab_loss.
  *   grad  nonzero for the backward pass, with dx or dw or both wanted.
  * Of x and w only the alignment counts; other arguments as below.

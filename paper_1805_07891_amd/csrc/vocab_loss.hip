@@ -768,9 +768,11 @@ __global__ __launch_bounds__(256) void target_logits(Operand x, Operand w, int k
 constexpr int kFinishRows = 16;
 
 // Joins the tiles' sums: 16 rows a block, their sums dealt to 64 groups of
-// threads, the rows' targets then to the waves.
-__global__ __launch_bounds__(1024) void finish_loss(const f32x2* part, int blocks, int64_t rows,
-                                                    Targets t, const float* pick, const int* alive,
+// threads, the rows' targets then to the waves.  Of a vocabulary in pieces this runs after
+// each: `before` (null after the first) holds the sums of earlier pieces, `carry` (null after the
+// last) takes them on.  The two may be the same array.
+__global__ __launch_bounds__(1024) void finish_loss(const f32x2* part, int blocks, const f32x2* before,
+                                                    f32x2* carry, int64_t rows, Targets t, const float* pick, const int* alive,
                                                     const float* entropy, float temperature,
                                                     float* loss, float* lse) {
     __shared__ f32x2 words[64][kFinishRows];
@@ -790,6 +792,7 @@ __global__ __launch_bounds__(1024) void finish_loss(const f32x2* part, int block
     auto above = [](f32x2 end, float z) { return (end.x - z) + end.y; };
     f32x2 s = {0.0f, 0.0f};
     if (first + in < rows) {
+        if (before && group == 0) s = before[first + in];
 #pragma unroll 4
         for (int b = group; b < blocks; b += 64) s = join(s, part[int64_t(b) * rows + first + in]);
     }
@@ -799,6 +802,10 @@ __global__ __launch_bounds__(1024) void finish_loss(const f32x2* part, int block
     for (int d = 32; d; d >>= 1) {
         if (group < d) words[group][in] = join(words[group][in], words[group + d][in]);
         __syncthreads();
+    }
+    if (carry) {
+        if (group == 0 && first + in < rows) carry[first + in] = words[0][in];
+        return;
     }
     if (group == 0 && first + in < rows) {
         const f32x2 all = words[0][in];
@@ -1447,7 +1454,7 @@ struct Layout {
     bool pack_x, pack_w;
     int planes;         // 2: fp32
     Plan logits_plan, dx_plan, dw_plan;  // cut by vocabulary, rows and vocabulary
-    int64_t blocks;     // of the vocabulary, in a piece: sums that a row leaves
+    int64_t blocks;     // of a piece: sums that a row leaves
     int counted;
     uint64_t* parts;
     int* arrived;
@@ -1455,7 +1462,7 @@ struct Layout {
     int *index, *teacher_alive, *alive, *row_exponent, *w_exponent, *largest, *largest_w;
     float *weight, *factor, *entropy, *pick, *scale_x, *scale_w, *part_x, *part_w;
     int64_t ld_p;       // of P and w's transpose
-    f32x2* part;
+    f32x2 *part, *carried;
     char *x, *w, *p, *xt, *wt;
     fp16* q;
 };
@@ -1492,7 +1499,8 @@ Layout lay_out(const VocabArgs& a, bool grad, int64_t piece, Arena* arena) {
     l.weight = arena->take<float>(entries, a.top > 0);
     l.teacher_alive = arena->take<int>(a.rows, a.top > 0);
     l.entropy = arena->take<float>(a.rows, a.top > 0);
-    l.part = arena->take<f32x2>(l.pieces * l.blocks * a.rows, !grad);
+    l.part = arena->take<f32x2>(l.blocks * a.rows, !grad);
+    l.carried = arena->take<f32x2>(a.rows, !grad && l.pieces > 1);
     l.alive = arena->take<int>(a.rows, grad);
     l.factor = arena->take<float>(a.rows, grad);
     l.pick = arena->take<float>(entries, !grad || a.top > 0);
@@ -1527,19 +1535,17 @@ int64_t bytes_of(const VocabArgs& a, bool grad, int64_t piece) {
     return count.used;
 }
 
-// The largest piece that fits, the pieces then made equal.
-int64_t choose_piece(const VocabArgs& a, bool grad, int64_t bytes) {
-    const int64_t all = up(a.vocab, kPieceAlign);
-    const int64_t most = std::min({all, kMostPiece, kMostLogits / a.rows / kPieceAlign * kPieceAlign});
-    if (bytes_of(a, grad, most) <= bytes) return most;
-    int64_t low = 1, high = most / kPieceAlign;  // in units of kPieceAlign
-    while (high - low > 1) {
-        const int64_t mid = (low + high) / 2;
-        (bytes_of(a, grad, mid * kPieceAlign) <= bytes ? low : high) = mid;
+// Calls run(piece) for equal pieces of the vocabulary, the largest first, each at least a
+// sixteenth smaller than the one before, until it returns true.
+template <typename F>
+void each_piece(const VocabArgs& a, F run) {
+    const int64_t units = up(a.vocab, kPieceAlign) / kPieceAlign;
+    int64_t most = std::min({units, kMostPiece / kPieceAlign, kMostLogits / a.rows / kPieceAlign});
+    while (true) {
+        const int64_t pieces = (units + most - 1) / most, size = (units + pieces - 1) / pieces;
+        if (run(size * kPieceAlign) || size == 1) return;
+        most = size - std::max<int64_t>(1, size / 16);
     }
-    const int64_t pieces = (all / kPieceAlign + low - 1) / low;
-    const int64_t even = (all / kPieceAlign + pieces - 1) / pieces * kPieceAlign;
-    return bytes_of(a, grad, even) <= bytes ? even : low * kPieceAlign;
 }
 
 // ---------------------------------------------------------- host: the passes
@@ -1660,12 +1666,12 @@ hipError_t gather_entries(const Operand& x, const Operand& w, const Product& p, 
 template <typename S, typename T>
 hipError_t loss_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
     hipError_t e = hipSuccess;
-    int blocks = 0;
-    for (int64_t i = 0; i < l.pieces && e == hipSuccess; ++i) {
+    for (int64_t i = 0; i < l.pieces; ++i) {
         const PieceAt at = piece_at(a, l, i);
+        int blocks = 0;
         e = launch_prepare<S>(a, l, i == 0, i == 0 ? pack_x(a, l) : PackArgs{},
                               pack_w(a, l, at.w, at.rows), RowsArgs{}, stream);
-        if (e != hipSuccess) break;
+        if (e != hipSuccess) return e;
         Product p;
         Logits z;
         logits_of(a, l, at, &p.c, &p.r, &p, &z);
@@ -1686,12 +1692,14 @@ hipError_t loss_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
             return a.top == 0 ? run_forward<T, kPlain>(shape, d, part, o, stream)
                               : run_forward<T, kTemperature>(shape, d, part, o, stream);
         });
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(finish_loss, dim3(unsigned((a.rows + kFinishRows - 1) / kFinishRows)),
+                           dim3(1024), 0, stream, l.part, blocks, i > 0 ? l.carried : nullptr,
+                           i + 1 < l.pieces ? l.carried : nullptr, a.rows, targets_of(a, l), l.pick,
+                           l.teacher_alive, l.entropy, a.temperature, a.loss, a.lse);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(finish_loss, dim3(unsigned((a.rows + kFinishRows - 1) / kFinishRows)),
-                       dim3(1024), 0, stream, l.part, blocks, a.rows, targets_of(a, l), l.pick,
-                       l.teacher_alive, l.entropy, a.temperature, a.loss, a.lse);
-    return hipGetLastError();
+    return e;
 }
 
 template <typename S, typename T>
@@ -1808,28 +1816,39 @@ hipError_t grad_pass(const VocabArgs& a, const Layout& l, hipStream_t stream) {
 
 }  // namespace
 
-void vocab_bytes(const VocabArgs& a, bool grad, int64_t* least, int64_t* best) {
-    if (a.rows == 0) {
-        if (least) *least = 0;
-        if (best) *best = 0;
-        return;
-    }
-    const int64_t one = bytes_of(a, grad, kPieceAlign);
-    if (least) *least = one;
-    if (best)
-        *best = std::max(one, bytes_of(a, grad, choose_piece(a, grad, std::max(one, kMostBytes))));
+int64_t vocab_piece(const VocabArgs& a, bool grad, int64_t bytes) {
+    int64_t found = 0;
+    each_piece(a, [&](int64_t piece) {
+        if (bytes_of(a, grad, piece) <= bytes) found = piece;
+        return found > 0;
+    });
+    return found;
 }
 
-hipError_t launch_vocab_loss(const VocabArgs& a, void* workspace, int64_t bytes, hipStream_t stream) {
-    if (a.rows == 0) return hipSuccess;
+// (Smaller pieces do not always take less: their smaller tiles leave a row more sums, and may be
+// done in parts.)
+void vocab_bytes(const VocabArgs& a, bool grad, int64_t* least, int64_t* best) {
+    int64_t few = 0, many = 0;
+    if (a.rows > 0)
+        each_piece(a, [&](int64_t piece) {
+            const int64_t n = bytes_of(a, grad, piece);
+            few = few == 0 ? n : std::min(few, n);
+            if (many == 0 && n <= kMostBytes) many = n;
+            return false;
+        });
+    if (least) *least = few;
+    if (best) *best = std::max(few, many);
+}
+
+hipError_t launch_vocab_loss(const VocabArgs& a, int64_t piece, void* workspace, hipStream_t stream) {
     Arena arena{static_cast<char*>(workspace)};
-    const Layout l = lay_out(a, false, choose_piece(a, false, bytes), &arena);
+    const Layout l = lay_out(a, false, piece, &arena);
     return a.type == kF32    ? loss_pass<float, fp16>(a, l, stream)
            : a.type == kBf16 ? loss_pass<bf16, bf16>(a, l, stream)
                              : loss_pass<fp16, fp16>(a, l, stream);
 }
 
-hipError_t launch_vocab_loss_grad(const VocabArgs& a, void* workspace, int64_t bytes,
+hipError_t launch_vocab_loss_grad(const VocabArgs& a, int64_t piece, void* workspace,
                                   hipStream_t stream) {
     if (a.rows == 0) {
         if (!a.dw || a.accumulate) return hipSuccess;
@@ -1839,7 +1858,7 @@ hipError_t launch_vocab_loss_grad(const VocabArgs& a, void* workspace, int64_t b
         return hipGetLastError();
     }
     Arena arena{static_cast<char*>(workspace)};
-    const Layout l = lay_out(a, true, choose_piece(a, true, bytes), &arena);
+    const Layout l = lay_out(a, true, piece, &arena);
     return a.type == kF32    ? grad_pass<float, fp16>(a, l, stream)
            : a.type == kBf16 ? grad_pass<bf16, bf16>(a, l, stream)
                              : grad_pass<fp16, fp16>(a, l, stream);

@@ -126,26 +126,34 @@ int check_teacher(int64_t rows, int top, float temperature) {
     return PHUB_OK;
 }
 
+// *piece: what the workspace is enough for.
+int check_vocab_workspace(const phub::VocabArgs& a, bool grad, const void* p, int64_t bytes,
+                          int64_t* piece) {
+    if (int rc = check_pointer("workspace", p, kWorkspaceAlign, true)) return rc;
+    *piece = phub::vocab_piece(a, grad, bytes);
+    if (*piece > 0) return PHUB_OK;
+    int64_t least = 0;
+    phub::vocab_bytes(a, grad, &least, nullptr);
+    return check_workspace(p, bytes, least);
+}
+
 int loss(const phub::VocabArgs& a, void* workspace, int64_t bytes, void* stream) {
     if (int rc = check_vocab(a, false)) return rc;
     if (a.rows == 0) return PHUB_OK;
-    int64_t least = 0;
-    phub::vocab_bytes(a, false, &least, nullptr);
-    if (int rc = check_workspace(workspace, bytes, least)) return rc;
-    return launched(phub::launch_vocab_loss(a, workspace, bytes, static_cast<hipStream_t>(stream)),
+    int64_t piece = 0;
+    if (int rc = check_vocab_workspace(a, false, workspace, bytes, &piece)) return rc;
+    return launched(phub::launch_vocab_loss(a, piece, workspace, static_cast<hipStream_t>(stream)),
                     "a loss over the vocabulary");
 }
 
 int loss_grad(const phub::VocabArgs& a, void* workspace, int64_t bytes, void* stream) {
     if (int rc = check_vocab(a, true)) return rc;
     if (!a.dx && !a.dw) return PHUB_OK;
-    if (a.rows > 0) {
-        int64_t least = 0;
-        phub::vocab_bytes(a, true, &least, nullptr);
-        if (int rc = check_workspace(workspace, bytes, least)) return rc;
-    }
+    int64_t piece = 0;
+    if (a.rows > 0)
+        if (int rc = check_vocab_workspace(a, true, workspace, bytes, &piece)) return rc;
     return launched(
-        phub::launch_vocab_loss_grad(a, workspace, bytes, static_cast<hipStream_t>(stream)),
+        phub::launch_vocab_loss_grad(a, piece, workspace, static_cast<hipStream_t>(stream)),
         "a loss's gradients over the vocabulary");
 }
 

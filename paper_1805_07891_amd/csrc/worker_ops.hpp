@@ -62,13 +62,15 @@ struct VocabArgs {
     bool accumulate;
 };
 
-// Bytes of workspace: the fewest that a call takes (the vocabulary in pieces
-// of one tile) and as many as it has use for.  Only the sizes, strides and the alignment of
-// x and w count.
+// Bytes of workspace: the fewest that a call takes and as many as it has use for.  Only the
+// sizes, strides and the alignment of x and w count.
 void vocab_bytes(const VocabArgs& a, bool grad, int64_t* least, int64_t* best);
-// workspace: 256-byte aligned, at least `least` bytes.
-hipError_t launch_vocab_loss(const VocabArgs& a, void* workspace, int64_t bytes, hipStream_t stream);
-hipError_t launch_vocab_loss_grad(const VocabArgs& a, void* workspace, int64_t bytes,
+// Vocabulary rows of the largest pieces that so many bytes are enough for; 0: too few.
+int64_t vocab_piece(const VocabArgs& a, bool grad, int64_t bytes);
+// piece: from vocab_piece; workspace: 256-byte aligned.
+hipError_t launch_vocab_loss(const VocabArgs& a, int64_t piece, void* workspace, hipStream_t stream);
+// (no rows: neither piece nor workspace count)
+hipError_t launch_vocab_loss_grad(const VocabArgs& a, int64_t piece, void* workspace,
                                   hipStream_t stream);
 
 }  // namespace phub
