@@ -702,7 +702,8 @@ __global__ __launch_bounds__(kProductThreads) void logits_forward(Product p, Log
 // The same for tiles of 256 x 256, whose epilogue has no registers for it: PAIRS (row,
 // entry) pairs a wave, rows of w gathered, of which the matrix instructions' 32 x 32
 // results give the diagonal.  The same instructions over the same k in the
-// same order give the same bits as the product's.  Fragments come straight from memory, as no two pairs share
+// same order give the same bits as the forward pass's product (the backward pass's, which has x for
+// its rows, takes fp32's two smaller products in the other order).  Fragments come straight from memory, as no two pairs share
 // rows of w, those of the next AHEAD instructions while this many are done.
 template <typename T, int PAIRS, int AHEAD>
 __global__ __launch_bounds__(256) void target_logits(Operand x, Operand w, int k, int segments,
