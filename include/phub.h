@@ -423,7 +423,10 @@ int phub_step_noalloc(int num_workers, int num_keys, const int64_t *key_elems,
  * the type that phub_push takes, and go where the caller says, such as
  * the buffer of a key; with `accumulate` they are added to what is there
  * (several micro-batches before one push).  Layer norm's weights are the fp32
- * values that phub_pull hands out.
+ * values that phub_pull hands out.  A job's step runs on the job's stream: order
+ * hip_stream after it before weights are read or a pushed buffer is written
+ * again, and the job's stream after hip_stream before the push (or push with
+ * an event).
  *
  * Like phub_step_noalloc, each works on the caller's memory, on hip_stream
  * (NULL = the null stream) of the current GPU, allocates nothing and does not

@@ -172,15 +172,21 @@ class TorchJob:
     def gradient(self, worker: int, key: int, *shape: int):
         """Key ``key`` in worker ``worker``'s attached arena, as a tensor of
         ``shape`` (default: flat): where an operator writes the gradient that
-        the worker pushes."""
+        the worker pushes.  Nothing is ordered here: a stream that writes it
+        first waits for the job's stream, whose last step reads it
+        (``stream.wait_stream(job.stream)``), and the job's stream waits for
+        the writer before the push, or the push is given the writer's event."""
         o, n = self.offsets[key], self.spec.key_elems[key]
         return self._grad_refs[worker][o:o + n].view(shape or (n,))
 
     def weights(self, key: int, *shape: int):
         """Key ``key``'s weights as phub_pull hands them out, as a tensor of
         ``shape`` (default: flat) that shares the job's memory and is read
-        only: ordered after earlier steps on the job's stream, changed by the
-        next step, gone with the job (which the tensor keeps)."""
+        only: changed by the next step, gone with the job (which the tensor
+        keeps).  Nothing is ordered here: a stream other than the job's waits
+        for it before it reads what the last step wrote
+        (``stream.wait_stream(job.stream)``), and the job's stream waits for
+        the reader before the next step."""
         n = self.spec.key_elems[key]
         ptr = self.lib.phub_pull(self.handle, key)
         return self.torch.as_tensor(_Pulled(self, ptr, n), device=self.device).view(shape or (n,))

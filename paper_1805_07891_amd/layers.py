@@ -6,8 +6,13 @@ these functions check the tensors and pass their pointers to the HIP library
 current stream of the tensors' device.  Weight gradients are fp32 and written
 (or added) where the caller says, such as ``TorchJob.gradient(worker, key)``,
 the part of a worker's arena that it pushes.
+A job has a stream of its own: the current stream waits for it before a call
+reads its weights or writes an arena, and it for the current stream before the
+push.  Autograd records nothing of these calls, whatever their inputs require:
+the gradients are what the backward calls return and write.
 
-Matrices are 2-D with adjacent columns; rows may be any distance apart.
+Matrices are 2-D with adjacent columns; their rows may lie further apart than
+they are long, but not overlap.
 ``workspace`` (a contiguous uint8 tensor, ``vocab_workspace``) is allocated
 where it is not given.  Calls that share one must be ordered on one stream.
 """
