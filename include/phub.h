@@ -456,7 +456,9 @@ enum phub_type { PHUB_F32 = 0, PHUB_BF16 = 1, PHUB_F16 = 2 };
  *   weight, bias  cols values; NULL: ones, zeros.
  *   mean, rstd    receive a value for each row (the backward pass takes
  *                 them); either may be NULL.
- * 0 <= rows < 2^30, 1 <= cols <= 2^20, eps >= 0 and finite.
+ * 0 <= rows < 2^30, 1 <= cols <= 2^20, eps >= 0 and finite.  The sums are fp32:
+ * a row whose sum of squares about its mean passes 2^128 (distances of 1e19)
+ * has no variance to speak of.
  */
 int phub_layer_norm(int type, int64_t rows, int64_t cols, const void *x, int64_t x_stride,
                     const float *weight, const float *bias, float eps, void *y, int64_t y_stride,
@@ -497,7 +499,8 @@ int phub_vocab_bytes(int type, int64_t rows, int64_t cols, int64_t vocab, const 
 
 /*
  * phub_vocab_loss - softmax cross entropy of each row's target over a
- * vocabulary, without keeping the rows x vocab logits z = x w^T:
+ * vocabulary, without keeping the rows x vocab logits z = x w^T (the
+ * workspace holds two values a row for each 128 or fewer of them):
  *     lse = log sum over v of exp z_v,   loss = lse - z_target
  *   x         rows x cols hidden states of `type`.
  *   w         vocab x cols weights of the same type.
@@ -526,6 +529,12 @@ int phub_vocab_loss(int type, int64_t rows, int64_t cols, int64_t vocab, const v
  *   dloss  a value for each row; NULL: ones.
  *   dx     rows x cols of `type`; NULL: not wanted.
  *   dw     vocab x cols fp32; NULL: not wanted.
+ * softmax(z) goes through the workspace, a piece of the vocabulary at a time:
+ * of *best bytes all of it at once, 6 bytes a logit (8 for fp32).  For dx of
+ * 16-bit types it is rounded to their type, for dx of fp32 and for dw to 22 bits.  A
+ * row's part in dw is right to that, and to 2^-38 of the largest product of a
+ * dloss and its row's largest value in x: rows whose product is that much smaller than
+ * another's add nothing to dw.
  */
 int phub_vocab_loss_grad(int type, int64_t rows, int64_t cols, int64_t vocab, const void *x,
                          int64_t x_stride, const void *w, int64_t w_stride, const int64_t *target,
