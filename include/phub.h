@@ -531,10 +531,11 @@ int phub_vocab_loss(int type, int64_t rows, int64_t cols, int64_t vocab, const v
  *   dw     vocab x cols fp32; NULL: not wanted.
  * softmax(z) goes through the workspace, a piece of the vocabulary at a time:
  * of *best bytes all of it at once, 6 bytes a logit (8 for fp32).  For dx of
- * 16-bit types it is rounded to their type, for dx of fp32 and for dw to 22 bits.  A
- * row's part in dw is right to that, and to 2^-38 of the largest product of a
- * dloss and its row's largest value in x: rows whose product is that much smaller than
- * another's add nothing to dw.
+ * 16-bit types softmax(z) less the target is rounded to their type (each entry's
+ * term is off by half a step of itself, also where the terms cancel), for dx
+ * of fp32 and for dw to 22 bits.  A row's part in dw is right to that, and to
+ * 2^-38 of the largest product of a dloss and its row's largest value in x:
+ * rows whose product is that much smaller than another's add nothing to dw.
  */
 int phub_vocab_loss_grad(int type, int64_t rows, int64_t cols, int64_t vocab, const void *x,
                          int64_t x_stride, const void *w, int64_t w_stride, const int64_t *target,

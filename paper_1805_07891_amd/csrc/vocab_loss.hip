@@ -23,10 +23,11 @@
 // entries are replaced by softmax(z) - q afterwards.  Two more products make
 // the gradients.
 // dx of bf16 and fp16 is rounded to 16 bits at the end, so P is of that
-// type: its rounding errors are independent from entry to entry and, weighted by the
-// entries, no larger than that last rounding (bf16, off 64 bits: 1.7e-3 of dx with the last rounding
-// alone, 2.0e-3 for 8192 rows of cross entropy over 32768 entries, 2.3e-3 for 4096 of
-// distillation over 65536; fp16 7.6e-4 and 7.7e-4).  A second plane would be dx's product again, 1.8 ms
+// type: its rounding errors are independent from entry to entry and half a step of each
+// entry's term, where the last rounding is half a step of their sum (bf16, off 64 bits: 1.7e-3 of dx
+// with the last rounding alone, 2.0e-3 for 8192 rows of cross entropy over 32768 entries, 2.3e-3 for 4096 of
+// distillation over 65536; 4.5e-3 where the rows of w have a part in common four times as large as the rest,
+// whose terms cancel; fp16 2.1e-4, 2.6e-4 and 6.2e-4 of such rows).  A second plane would be dx's product again, 1.8 ms
 // beside 9.8 for the first of these.  dw is fp32 (what a worker pushes), so Q is two fp16
 // planes, 22 bits, and takes two products: one bf16 plane would leave 2e-3
 // of dw wrong.  x in the product for dw is fp16 too, scaled by its row's
