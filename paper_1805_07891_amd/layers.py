@@ -160,7 +160,8 @@ def layer_norm_grad(dy, x, weight, mean, rstd, dweight=None, dbias=None, accumul
 def vocab_workspace(x, w, top: int = 0, grad: bool = True, most: Optional[int] = None, lib=None):
     """A workspace for the losses below (``top``: the teacher's entries a row,
     0 for targets; ``grad``: for the backward pass): as large as a call has
-    use for, or of ``most`` bytes if that is less and enough."""
+    use for, or of ``most`` bytes if that is less and enough.  The backward
+    pass's is enough for the forward pass of the same sizes."""
     least, best = _library(lib).phub_vocab_bytes(*_sizes(x, w), top, 1 if grad else 0)
     n = best if most is None else max(least, min(best, int(most)))
     return _empty(n, dtype=torch.uint8, device=x.device)
